@@ -392,6 +392,80 @@ EPICACHE_API int epicache_match_queries(const float* queries, const float* centr
 EPICACHE_API int epicache_layer_budgets(const double* sensitivity, int32_t n_layers, double alpha,
                                         int32_t budget, int32_t* budgets_out);
 
+/* ---- A cache in 8 bits, for decoding with the rows that eviction leaves.
+ *
+ * K and V are held as OCP e4m3 codes with one float32 scale per block of `block_tokens` rows and KV head (block j: rows
+ * j * block_tokens .. (j + 1) * block_tokens - 1); a row's values are code * scale.  The scales that the library writes are
+ * powers of two, so codes change only by the rounding of what falls below the smallest step; any positive finite scale may be
+ * given.  Beside them, for every row, the attention weight that it has received so far (`weight`) and its position in
+ * the sequence (`position`), which eviction goes by.
+ *
+ * A step is append, attention, evict with one epicache_params.  In all three calls the rows of a head (b, h) are
+ *   n_ctx_opt ? clamp(n_ctx_opt[b * n_kv_heads + h], 0, n_cached) : n_cached   old rows, and n_block new ones behind them;
+ * n_cached + n_block <= capacity.  What lies behind them is neither read nor written.
+ * The struct is read on the host during the call; the arrays are DEVICE memory, 16-byte aligned, the codes' strides
+ * multiples of 16.  Each call checks the fields of `params` that it names, and n_batch, n_q_heads, n_kv_heads, head_dim
+ * (here a multiple of 16, 16..256), n_cached, n_block, dtype; `reduce` is not used.  Same conventions as above: a call enqueues
+ * on `hip_stream`, of the current device, and can be captured. */
+typedef struct epicache_kv8 {
+  uint32_t struct_size;   /* sizeof(epicache_kv8), checked                                            */
+  int32_t block_tokens;   /* rows that share a scale: 16, 32, 64 or 128                                */
+  int32_t capacity;       /* rows per head that the arrays hold, >= 1                                  */
+  int32_t reserved;       /* must be 0                                                                 */
+  void* k;                /* e4m3 codes [n_batch, n_kv_heads, capacity, head_dim], strides stride_*   */
+  void* v;                /* the same layout, another buffer                                           */
+  float* k_scale;         /* [n_batch, n_kv_heads, ceil(capacity / block_tokens)], strides scale_*     */
+  float* v_scale;
+  float* weight;          /* [n_batch, n_kv_heads, capacity], strides row_*; NULL: none (append, attention) */
+  int32_t* position;      /* the same layout; NULL: none, a row's index stands for it                  */
+  int64_t stride_b, stride_h, stride_t;  /* codes, in bytes; head_dim is contiguous                     */
+  int64_t scale_stride_b, scale_stride_h;
+  int64_t row_stride_b, row_stride_h;
+} epicache_kv8;
+
+/* Bytes of device workspace that any of the three calls needs for `params` and `cache` (whose arrays may be NULL here).
+ * Pure host computation. */
+EPICACHE_API int epicache_kv8_workspace_size(const epicache_params* params, const epicache_kv8* cache, size_t* bytes_out);
+
+/* The n_block rows k_new, v_new [n_batch, n_kv_heads, n_block, head_dim] (dtype; strides kv_stride_* of `params`, which
+ * both share) are put behind every head's old rows.  A block's scale is the smallest power of two, at least 2^-126, that brings
+ * its largest new magnitude to at most 448, and no smaller than what it was if it holds old rows; where it has become
+ * larger these are rounded again (code * old scale / new scale).  A code is the e4m3 value nearest to value / scale, ties to
+ * even; infinities and NaNs become the NaN code (0x7f) and have no part in the scale.
+ * The new rows' weight is set to 0 and their position to first_position_opt[b] + 0, 1, .. ([n_batch] int32), or to their row
+ * index where that is NULL.  n_ctx_opt is only read.  Uses of params: n_block (0: nothing to do), kv_stride_*. */
+EPICACHE_API int epicache_kv8_append(const epicache_params* params, const epicache_kv8* cache, const void* k_new,
+                                     const void* v_new, const int32_t* n_ctx_opt, const int32_t* first_position_opt,
+                                     void* hip_stream);
+
+/* For every query t of every query head: out = sum_i softmax_i(scale * q_t . k_i) v_i and lse_out = log of the sum of
+ * exp(scale * q_t . k_i), over the rows of its KV head; causal_patch = 1: the queries are the n_block new rows' own
+ * (patch_len must be n_block), and query t sees the rows up to its own.  patch_len = 1 is a decoding step.
+ * accumulate = 1: weight[b, h, i] of every row i += the softmax weights that it received from the
+ * n_q_heads / n_kv_heads * patch_len queries of its head, summed in a fixed order.
+ * A query without a row, or whose logits are all -inf, gets out = 0 and lse = -inf and adds nothing.
+ * In: q [n_batch, n_q_heads, patch_len, head_dim] (dtype, strides q_stride_*).  Out, dense: out as q, in dtype; lse_out float32.
+ * Products of the decoded values on the matrix cores, sums and exponentials in fp32; logits above -1e30.
+ * Uses of params: patch_len, softmax_scale, causal_patch, q_stride_*. */
+EPICACHE_API int epicache_kv8_attention(const epicache_params* params, const epicache_kv8* cache, const void* q,
+                                        const int32_t* n_ctx_opt, int32_t accumulate, void* out, float* lse_out,
+                                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Eviction by accumulated attention weight.  Every head keeps K = min(M, its rows) rows, M = budgets_opt ?
+ * clamp(budgets_opt[b], 0, budget) : budget (budgets_opt [n_batch] int32): first the n_recent latest ones (position above the head's
+ * highest minus n_recent), then those of the largest weight (ordered as epicache_topk's scores, every positive NaN alike); ties to the
+ * lower row.  The kept rows below K stay where they are, and those from K on move, in ascending order, into the places below K of the
+ * rows that go, in ascending order: codes, weight and position.  So few rows move, and the order of the cache is no
+ * longer that of the positions.  The scale of a block that takes rows in becomes, as in epicache_kv8_append, the
+ * larger of what they need and of what it was if rows stay in it.  Rows from K on are left as they were, but their block's scale
+ * may be a new one where K is inside a block.
+ * Out: n_kept [n_batch, n_kv_heads] int32 (may be n_ctx_opt's array); row_from_opt, if not NULL, [n_batch, n_kv_heads,
+ * min(budget, n_cached + n_block)] int32: the row that row i was, -1 from K on.
+ * 0 <= n_recent <= budget.  cache->weight must be given.  Uses of params: budget. */
+EPICACHE_API int epicache_kv8_evict(const epicache_params* params, const epicache_kv8* cache, int32_t n_recent,
+                                    const int32_t* n_ctx_opt, const int32_t* budgets_opt, int32_t* n_kept,
+                                    int32_t* row_from_opt, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, NUL-terminated description of an epicache_status value. */
 EPICACHE_API const char* epicache_status_string(int status);
 

@@ -32,7 +32,9 @@ ENTRY_POINTS = (
     "epicache_kvzip_workspace_size", "epicache_score_kvzip", "epicache_evict_step_kvzip", "epicache_score_keydiff", "epicache_patch_attention",
     "epicache_patch_attention_ragged",
     "epicache_attn_workspace_size", "epicache_evict_step_attn",
-    "epicache_episode_medoids", "epicache_match_queries", "epicache_status_string", "epicache_version",
+    "epicache_episode_medoids", "epicache_match_queries",
+    "epicache_kv8_workspace_size", "epicache_kv8_append", "epicache_kv8_attention", "epicache_kv8_evict",
+    "epicache_status_string", "epicache_version",
 )
 _INT_RETURNING = ENTRY_POINTS[:-2]
 
@@ -60,6 +62,29 @@ class Params(ctypes.Structure):
         ("kv_stride_b", ctypes.c_int64),
         ("kv_stride_h", ctypes.c_int64),
         ("kv_stride_t", ctypes.c_int64),
+    ]
+
+
+class Kv8(ctypes.Structure):
+    """struct epicache_kv8.  One made by make_kv8 keeps its tensors alive."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("block_tokens", ctypes.c_int32),
+        ("capacity", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("k_scale", ctypes.c_void_p),
+        ("v_scale", ctypes.c_void_p),
+        ("weight", ctypes.c_void_p),
+        ("position", ctypes.c_void_p),
+        ("stride_b", ctypes.c_int64),
+        ("stride_h", ctypes.c_int64),
+        ("stride_t", ctypes.c_int64),
+        ("scale_stride_b", ctypes.c_int64),
+        ("scale_stride_h", ctypes.c_int64),
+        ("row_stride_b", ctypes.c_int64),
+        ("row_stride_h", ctypes.c_int64),
     ]
 
 
@@ -123,6 +148,11 @@ def load() -> ctypes.CDLL:
     lib.epicache_evict_step_attn.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.epicache_episode_medoids.argtypes = [vp, vp, i32c, i32c, i32c, vp, vp, vp]
     lib.epicache_match_queries.argtypes = [vp, vp, i32c, i32c, i32c, ctypes.c_float, vp, vp, vp]
+    kp = ctypes.POINTER(Kv8)
+    lib.epicache_kv8_workspace_size.argtypes = [pp, kp, ctypes.POINTER(sz)]
+    lib.epicache_kv8_append.argtypes = [pp, kp, vp, vp, vp, vp, vp]
+    lib.epicache_kv8_attention.argtypes = [pp, kp, vp, vp, i32c, vp, vp, vp, sz, vp]
+    lib.epicache_kv8_evict.argtypes = [pp, kp, i32c, vp, vp, vp, vp, vp, sz, vp]
     for name in _INT_RETURNING:
         getattr(lib, name).restype = i32
     lib.epicache_status_string.argtypes = [i32]
@@ -375,6 +405,67 @@ def epicache_match_queries(queries, centroids, tau: float, episode, cosine=None)
     assert queries.dtype == torch.float32 and queries.is_contiguous() and centroids.is_contiguous()
     _check(load().epicache_match_queries(_ptr(queries), _ptr(centroids), nq, centroids.shape[0], D, float(tau),
                                          _ptr(episode), _ptr(cosine), _stream()), "epicache_match_queries")
+
+
+def make_kv8(k, v, k_scale, v_scale, block_tokens: int, weight=None, position=None) -> Kv8:
+    """epicache_kv8 of an 8-bit cache: k, v [nb,Hkv,C,d] uint8 or float8_e4m3fn, k_scale, v_scale [nb,Hkv,ceil(C/block_tokens)]
+    float32, weight [nb,Hkv,C] float32, position [nb,Hkv,C] int32.  K and V share strides, and so do the pairs behind them."""
+    nb, H, C, d = k.shape
+    pair = (weight, position)
+    rows = next((t for t in pair if t is not None), None)
+    if not (k.dtype == v.dtype and k.dtype in (torch.uint8, torch.float8_e4m3fn) and k_scale.dtype == v_scale.dtype == torch.float32
+            and (weight is None or weight.dtype == torch.float32) and (position is None or position.dtype == torch.int32)):
+        raise ValueError("make_kv8: codes are uint8 or float8_e4m3fn, scales and weights float32, positions int32")
+    if not (v.shape == k.shape and v.stride() == k.stride() and k.stride(3) == 1 and
+            k_scale.shape == v_scale.shape == (nb, H, -(-C // block_tokens)) and v_scale.stride() == k_scale.stride() and
+            (k_scale.shape[2] == 1 or k_scale.stride(2) == 1) and
+            all(t is None or (t.shape == (nb, H, C) and t.stride() == rows.stride() and (C == 1 or t.stride(2) == 1)) for t in pair)):
+        raise ValueError("make_kv8: shapes or strides do not belong together")
+    row_strides = (0, 0) if rows is None else rows.stride()[:2]
+    kv8 = Kv8(ctypes.sizeof(Kv8), block_tokens, C, 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+              None if weight is None else weight.data_ptr(), None if position is None else position.data_ptr(), *k.stride()[:3],
+              *k_scale.stride()[:2], *row_strides)
+    kv8.tensors = (k, v, k_scale, v_scale, weight, position)
+    return kv8
+
+
+def alloc_kv8(n_batch: int, n_kv_heads: int, capacity: int, head_dim: int, block_tokens: int = 32, device="cuda"):
+    """(k, v, k_scale, v_scale, weight, position) of an empty 8-bit cache, in make_kv8's order but for block_tokens."""
+    shape = (n_batch, n_kv_heads, capacity)
+    blocks = (n_batch, n_kv_heads, -(-capacity // block_tokens))
+    codes = [torch.zeros((*shape, head_dim), dtype=torch.float8_e4m3fn, device=device) for _ in range(2)]
+    scales = [torch.ones(blocks, dtype=torch.float32, device=device) for _ in range(2)]
+    return (*codes, *scales, torch.zeros(shape, dtype=torch.float32, device=device),
+            torch.zeros(shape, dtype=torch.int32, device=device))
+
+
+def epicache_kv8_workspace_size(params: Params, kv8: Kv8) -> int:
+    out = ctypes.c_size_t(0)
+    _check(load().epicache_kv8_workspace_size(ctypes.byref(params), ctypes.byref(kv8), ctypes.byref(out)),
+           "epicache_kv8_workspace_size")
+    return out.value
+
+
+def alloc_kv8_workspace(params: Params, kv8: Kv8, device="cuda") -> torch.Tensor:
+    """A workspace of epicache_kv8_workspace_size(params, kv8)."""
+    return torch.empty(max(epicache_kv8_workspace_size(params, kv8), 256), dtype=torch.uint8, device=device)
+
+
+def epicache_kv8_append(params: Params, kv8: Kv8, k_new, v_new, n_ctx=None, first_position=None) -> None:
+    _check(load().epicache_kv8_append(ctypes.byref(params), ctypes.byref(kv8), _ptr(k_new), _ptr(v_new), _ptr(n_ctx),
+                                      _ptr(first_position), _stream()), "epicache_kv8_append")
+
+
+def epicache_kv8_attention(params: Params, kv8: Kv8, q, n_ctx, out, lse_out, workspace, accumulate: bool = False) -> None:
+    _check(load().epicache_kv8_attention(ctypes.byref(params), ctypes.byref(kv8), _ptr(q), _ptr(n_ctx), int(accumulate),
+                                         _ptr(out), _ptr(lse_out), _ptr(workspace),
+                                         0 if workspace is None else workspace.numel(), _stream()), "epicache_kv8_attention")
+
+
+def epicache_kv8_evict(params: Params, kv8: Kv8, n_recent: int, n_ctx, budgets, n_kept, workspace, row_from=None) -> None:
+    _check(load().epicache_kv8_evict(ctypes.byref(params), ctypes.byref(kv8), int(n_recent), _ptr(n_ctx), _ptr(budgets),
+                                     _ptr(n_kept), _ptr(row_from), _ptr(workspace), workspace.numel(), _stream()),
+           "epicache_kv8_evict")
 
 
 def epicache_layer_budgets(sensitivity, alpha: float, budget: int):
