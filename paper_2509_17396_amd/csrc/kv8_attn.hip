@@ -10,113 +10,8 @@
 namespace epicache {
 namespace {
 
-__device__ __forceinline__ float to_float(__hip_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ void put(__hip_bfloat16& to, float x) { to = __float2bfloat16(x); }
-__device__ __forceinline__ void put(float& to, float x) { to = x; }
-
-__device__ __forceinline__ float block_reduce(float x, bool is_max, float* lds) {
-  for (int s = 32; s >= 1; s >>= 1) {
-    const float y = __shfl_xor(x, s);
-    x = is_max ? fmaxf(x, y) : x + y;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return is_max ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3])) : (lds[0] + lds[1]) + (lds[2] + lds[3]);
-}
-
-// One workgroup per query: 256 keys at a time, a key per thread for the logits, a column per thread for the output.
-template <typename T>
-__global__ __launch_bounds__(256) void kv8_attention_rows(Kv8Plan pl, const T* __restrict__ q, T* __restrict__ out,
-                                                          float* __restrict__ lse, float2* __restrict__ stats) {
-  __shared__ float qs[256], w[256], red[4];
-  const int tid = threadIdx.x;
-  const size_t orow = blockIdx.x;
-  const int t = (int)(orow % pl.p), hq = (int)(orow / pl.p % pl.Hq), b = (int)(orow / pl.p / pl.Hq), h = hq / pl.G;
-  const int bh = b * pl.Hkv + h;
-  const int old = kv8_old_rows(pl, bh), n = pl.causal ? old + t + 1 : old + pl.n_block;
-  const uint8_t* k = pl.k + b * pl.sb + h * pl.sh;
-  const uint8_t* v = pl.v + b * pl.sb + h * pl.sh;
-  const float* ks = pl.k_scale + b * pl.ssb + h * pl.ssh;
-  const float* vs = pl.v_scale + b * pl.ssb + h * pl.ssh;
-  if (tid < pl.d) qs[tid] = to_float(q[b * pl.qsb + hq * pl.qsh + t * pl.qst + tid]);
-  __syncthreads();
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  for (int k0 = 0; k0 < n; k0 += 256) {
-    const int i = k0 + tid;
-    float z = -INFINITY;
-    if (i < n) {
-      float dot = 0.f;
-      for (int c = 0; c < pl.d; c += 4) {
-        float x[4];
-        decode4(*reinterpret_cast<const uint32_t*>(k + (int64_t)i * pl.st + c), x);
-        for (int j = 0; j < 4; j++) dot = fmaf(qs[c + j], x[j], dot);
-      }
-      z = dot * ks[i >> pl.block_shift] * pl.c2;
-    }
-    const float mn = fmaxf(m, block_reduce(z, true, red));
-    const float e = z == -INFINITY ? 0.f : exp2f(z - mn), corr = m == mn ? 1.f : exp2f(m - mn);
-    l = l * corr + block_reduce(e, false, red);
-    acc *= corr;
-    m = mn;
-    w[tid] = e;
-    __syncthreads();
-    if (tid < pl.d)
-      for (int j = 0; j < min(256, n - k0); j++) {
-        float x[4];
-        decode4(v[(int64_t)(k0 + j) * pl.st + tid], x);
-        acc = fmaf(w[j] * vs[(k0 + j) >> pl.block_shift], x[0], acc);
-      }
-    __syncthreads();
-  }
-  const bool any = l > 0.f || l != l;
-  if (tid < pl.d) put(out[orow * pl.d + tid], any ? acc / l : 0.f);
-  if (tid == 0) {
-    lse[orow] = any ? (m + log2f(l)) * 0.69314718055994530942f : -INFINITY;
-    if (stats) stats[orow] = make_float2(m, any ? 1.f / l : 0.f);
-  }
-}
-
-// weight += the softmax weights, a key per thread, the queries of its head one after the other.
-template <typename T>
-__global__ __launch_bounds__(256) void kv8_accumulate_keys(Kv8Plan pl, const T* __restrict__ q, const float2* __restrict__ stats) {
-  const int bh = blockIdx.y, b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
-  const int old = kv8_old_rows(pl, bh), n = old + pl.n_block, i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  const uint8_t* k = pl.k + b * pl.sb + h * pl.sh + (int64_t)i * pl.st;
-  const float scale = pl.k_scale[b * pl.ssb + h * pl.ssh + (i >> pl.block_shift)];
-  float sum = 0.f;
-  for (int r = 0; r < pl.R; r++) {
-    const int g = r / pl.p, t = r - g * pl.p;
-    if (pl.causal && i > old + t) continue;
-    const T* row = q + b * pl.qsb + (h * pl.G + g) * pl.qsh + t * pl.qst;
-    float dot = 0.f;
-    for (int c = 0; c < pl.d; c += 4) {
-      float x[4];
-      decode4(*reinterpret_cast<const uint32_t*>(k + c), x);
-      for (int j = 0; j < 4; j++) dot = fmaf(to_float(row[c + j]), x[j], dot);
-    }
-    const float2 s = stats[((size_t)b * pl.Hq + h * pl.G + g) * pl.p + t];
-    if (s.y != 0.f) sum += exp2f(dot * scale * pl.c2 - s.x) * s.y;
-  }
-  pl.weight[b * pl.rsb + h * pl.rsh + i] += sum;
-}
-
-template <typename T>
-hipError_t launch(const Kv8Plan& pl, const void* q, void* out, float* lse, float2* stats, hipStream_t stream) {
-  hipLaunchKernelGGL(kv8_attention_rows<T>, dim3((unsigned)((size_t)pl.nb * pl.Hq * pl.p)), dim3(256), 0, stream, pl,
-                     static_cast<const T*>(q), static_cast<T*>(out), lse, stats);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !pl.accumulate) return e;
-  hipLaunchKernelGGL(kv8_accumulate_keys<T>, dim3((pl.n_cached + pl.n_block + 255) / 256, pl.nb * pl.Hkv), dim3(256), 0, stream,
-                     pl, static_cast<const T*>(q), stats);
-  return hipGetLastError();
-}
-
 // ---- Few query rows per KV head (decoding): every wave streams its own keys through registers.
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
@@ -147,10 +42,38 @@ __device__ __forceinline__ void cut_pair(uint32_t (&p)[PARTS], float a, float b)
   }
 }
 
+// Eight fp32 values as three operand parts; not ok: zeros.
+__device__ __forceinline__ void cut_row8(bf16x8 (&f)[3], const float* row, bool ok) {
+  float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (ok) {
+    const float4 a = reinterpret_cast<const float4*>(row)[0], b = reinterpret_cast<const float4*>(row)[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+  u32x4 u[3];
+#pragma unroll
+  for (int j = 0; j < 4; j++) {
+    uint32_t p[3];
+    cut_pair<3>(p, x[2 * j], x[2 * j + 1]);
+    // nothing is left of an infinity or a NaN, and a NaN stays one
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+      const float y = x[2 * j + e];
+      if (is_finite(y)) continue;
+      const uint32_t top = (y != y ? 0x7fc0u : __float_as_uint(y) >> 16) << 16 * e, keep = e ? 0xffffu : 0xffff0000u;
+      p[0] = (p[0] & keep) | top, p[1] &= keep, p[2] &= keep;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; i++) u[i][j] = p[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 3; i++) f[i] = __builtin_bit_cast(bf16x8, u[i]);
+}
+
 // e4m3 codes 2 i, 2 i + 1 of a dword as bf16, which holds them exactly.
+// `scale`: a power of two to be multiplied with.
 template <int HIGH>
-__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t u) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, 1.0f, HIGH != 0));
+__device__ __forceinline__ uint32_t codes_to_bf16(uint32_t u, float scale = 1.f) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, scale, HIGH != 0));
 }
 __device__ __forceinline__ bf16x8 codes_to_frag(uint32_t lo, uint32_t hi) {
   const u32x4 u = {codes_to_bf16<0>(lo), codes_to_bf16<1>(lo), codes_to_bf16<0>(hi), codes_to_bf16<1>(hi)};
@@ -178,34 +101,14 @@ __device__ __forceinline__ void load_query(bf16x8 (&f)[3][2 * NCH], const float*
 #pragma unroll
     for (int s = 0; s < 2; s++) {
       const int at = (4 * c + g) * 16 + 8 * s;
-      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (ok && at < d) {
-        const float4 a = reinterpret_cast<const float4*>(row + at)[0], b = reinterpret_cast<const float4*>(row + at)[1];
-        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-      }
-      u32x4 u[3];
+      bf16x8 parts[3];
+      cut_row8(parts, row + at, ok && at < d);
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        uint32_t p[3];
-        cut_pair<3>(p, x[2 * j], x[2 * j + 1]);
-        // nothing is left of an infinity or a NaN, and a NaN stays one
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          const float y = x[2 * j + e];
-          if (is_finite(y)) continue;
-          const uint32_t top = (y != y ? 0x7fc0u : __float_as_uint(y) >> 16) << 16 * e, keep = e ? 0xffffu : 0xffff0000u;
-          p[0] = (p[0] & keep) | top, p[1] &= keep, p[2] &= keep;
-        }
-#pragma unroll
-        for (int i = 0; i < 3; i++) u[i][j] = p[i];
-      }
-#pragma unroll
-      for (int i = 0; i < 3; i++) f[i][2 * c + s] = __builtin_bit_cast(bf16x8, u[i]);
+      for (int i = 0; i < 3; i++) f[i][2 * c + s] = parts[i];
     }
 }
 
 __device__ __forceinline__ void store4(__hip_bfloat16* to, const float (&x)[4]) {
-  typedef __attribute__((ext_vector_type(2))) float f32x2;
   uint2 u;
   u.x = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
   u.y = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2], x[3]}), bf16x2));
@@ -222,12 +125,14 @@ struct Step {
   float ks[2], vs[2];
 };
 
+// 0x80 where a byte is the NaN code, 0x7f or 0xff.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t u) { return ((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
 // NaN codes of V in a step that some rows see and others do not: the rows that see one get a NaN in its column, and the code is
 // taken out, since a weight of 0 times it would make one of the others' columns too.  Whether a row sees one is a product of
 // zeros and ones.
 template <int NCH, int NR>
 __device__ __forceinline__ void not_numbers(Step<NCH>& s, f32x4 (&acc)[NR][4 * NCH], int key0, int g, const int (&last)[NR]) {
-  auto nan_bytes = [](uint32_t u) { return ((u & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };  // 0x80 where the byte is 0x7f or 0xff
   uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < 8; i++)
@@ -596,6 +501,503 @@ __global__ __launch_bounds__(256) void kv8_join_tokens(Kv8Plan pl, T* __restrict
     if (key + i < n) to[i] += w[i];
 }
 
+// ---- Many query rows per KV head (patches, prefilled blocks): tiles of keys through LDS, shared by the waves of a workgroup.
+//
+// A wave owns 32 query rows.  Tiles of 64 rows of K and V come from memory as codes, one tile ahead, are decoded to bf16 (exactly,
+// with their scale where it is a power of two) by whoever fetched them and lie in LDS double buffered, K as the scoring kernels have it and
+// V as the patch attention's transposing loads want it.  Per 32 keys: S^T = K Q^T, an online softmax, O^T += V^T P^T.
+
+struct BlockRoom {
+  int splits, split_tiles;  // workgroups that share the keys of a row, and the tiles of each
+  float2* rows;             // [heads][R]: reference and 1 / sum, where weights are accumulated
+  float2* stats;            // [heads][splits][R], where there are several: reference and sum
+  float* records;           // [heads][splits][R][d]: outputs before the division
+};
+
+constexpr int kBlockKeys = 64;
+
+// Waves of a workgroup: no more than have rows.
+int block_waves(const Kv8Plan& pl) { return pl.R <= 64 ? 2 : 4; }
+
+__device__ __forceinline__ bool folds(float scale) {  // into the exponent of a decoded value
+  const uint32_t u = __float_as_uint(scale);
+  return (u & 0x7fffffu) == 0 && u != 0;
+}
+
+// Thread's share of a tile on its way to LDS: 16-code chunks tid, tid + NT, .. of the tile's rows, K and V.
+template <int HD, int NT>
+struct TileCodes {
+  static constexpr int kPer = kBlockKeys * (HD / 16) / NT;
+  uint4 k[kPer], v[kPer];
+  float ks[kPer], vs[kPer];
+};
+
+constexpr int block_occupancy(size_t elem, int hd) { return elem == 2 && hd <= 128 ? 2 : 1; }
+
+__device__ __forceinline__ uint4 codes_to_bf16x8(uint32_t lo, uint32_t hi, float scale) {
+  return make_uint4(codes_to_bf16<0>(lo, scale), codes_to_bf16<1>(lo, scale), codes_to_bf16<0>(hi, scale), codes_to_bf16<1>(hi, scale));
+}
+
+// The 8 values of chunks hi, 2 + hi, .. of a row as operand parts; zeros behind d.
+template <int KS>
+__device__ __forceinline__ void load_rows(bf16x8 (&f)[1][KS], const __hip_bfloat16* row, int hi, int d) {
+  load_row_frags<KS>(f[0], reinterpret_cast<const bf16_t*>(row), hi, d);
+}
+template <int KS>
+__device__ __forceinline__ void load_rows(bf16x8 (&f)[3][KS], const float* row, int hi, int d) {
+#pragma unroll
+  for (int j = 0; j < KS; j++) {
+    bf16x8 parts[3];
+    const int at = (2 * j + hi) * 8;
+    cut_row8(parts, row + at, at < d);
+#pragma unroll
+    for (int i = 0; i < 3; i++) f[i][j] = parts[i];
+  }
+}
+
+// Rows from .. to - 1 of a head: how many keys each of them sees at least, and how many at most.
+__device__ __forceinline__ void rows_see(const Kv8Plan& pl, int old, int n, int from, int to, int& least, int& most) {
+  least = most = n;
+  if (!pl.causal) return;
+  int ga, ta, gb, tb;
+  head_and_token(pl.p, pl.inv_p, min(from, pl.R - 1), ga, ta);
+  head_and_token(pl.p, pl.inv_p, min(to, pl.R) - 1, gb, tb);
+  least = old + 1 + (ga == gb ? ta : 0), most = old + 1 + (ga == gb ? tb : pl.p - 1);
+}
+
+// V^T operand of the NaN codes among 8 keys (key + 0 .. 3, key + 8 .. 11) of one column: ones.
+__device__ __forceinline__ bf16x8 nan_frag(const uint8_t* v, uint32_t pitch, int key, int n) {
+  u32x4 u = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < 8; j++) {
+    const int at = key + (j & 3) + (j >> 2) * 8;
+    if (at < n && (v[(int64_t)at * pitch] & 0x7f) == 0x7f) u[j >> 1] |= 0x3f80u << 16 * (j & 1);
+  }
+  return __builtin_bit_cast(bf16x8, u);
+}
+
+// HD: row layout in LDS; KS 16-element steps of Q K^T, DB 32-column blocks of the output.
+template <typename T, int HD, int KS, int DB, int NW>
+__global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_attention_block(
+    Kv8Plan pl, const T* __restrict__ q, T* __restrict__ out, float* __restrict__ lse, BlockRoom room) {
+  using TL = Tile<HD>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int PARTS = F32 ? 3 : 1, NT = NW * 64;
+  constexpr int kTile = kBlockKeys * TL::kRowBytes;
+  using Codes = TileCodes<HD, NT>;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // K, K, V, V, then
+  float(*rest)[2][4] = reinterpret_cast<float(*)[2][4]>(smem + 4 * kTile);  // [buffer][K, V][16 keys]: what scales have not been folded
+  int* nan_seen = reinterpret_cast<int*>(smem + 4 * kTile + 64);            // [buffer]: the tile there from whose V NaN codes have been taken out
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hi = lane >> 5;
+  // XCD-aware ids: the row blocks of one head and split read the same keys and land on one XCD; the last rows, which see most, first
+  const int n_rb = gridDim.x >> 3, rb = n_rb - 1 - (blockIdx.x >> 3);
+  const int unit = blockIdx.y * 8 + (blockIdx.x & 7);
+  if (unit >= pl.nb * pl.Hkv * room.splits) return;
+  const int bh = unit / room.splits, split = unit - bh * room.splits;
+  const int b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
+  const int old = kv8_old_rows(pl, bh), n = old + pl.n_block;
+
+  const int first_row = rb * 32 * NW, row0 = first_row + wave * 32, r = row0 + l32;
+  const bool active = row0 < pl.R, row_ok = r < pl.R;
+  int g_row, t_row;
+  head_and_token(pl.p, pl.inv_p, min(r, pl.R - 1), g_row, t_row);
+  const int last_key = pl.causal ? old + t_row : n - 1;
+  int all_see, any_sees, wave_all, wave_any;
+  rows_see(pl, old, n, first_row, first_row + 32 * NW, all_see, any_sees);
+  rows_see(pl, old, n, row0, row0 + 32, wave_all, wave_any);
+  const int tiles = (any_sees + kBlockKeys - 1) / kBlockKeys;
+  const int first_tile = split * room.split_tiles, end_tile = room.splits == 1 ? tiles : min(tiles, first_tile + room.split_tiles);
+
+  bf16x8 qf[PARTS][KS];
+  load_rows<KS>(qf, q + b * pl.qsb + (int64_t)(h * pl.G + g_row) * pl.qsh + (int64_t)t_row * pl.qst, hi, pl.d);
+
+  const uint8_t* kbase = pl.k + b * pl.sb + h * pl.sh;
+  const uint8_t* vbase = pl.v + b * pl.sb + h * pl.sh;
+  const float* ks = pl.k_scale + b * pl.ssb + h * pl.ssh;
+  const float* vs = pl.v_scale + b * pl.ssb + h * pl.ssh;
+  const uint32_t pitch = (uint32_t)pl.st;
+
+  // a row of the tile has HD / 16 chunks, of which the first d / 16 are there
+  auto fetch = [&](Codes& c, int t) {
+    const int key0 = t * kBlockKeys;
+#pragma unroll
+    for (int i = 0; i < Codes::kPer; i++) {
+      const int at = tid + i * NT, row = at / (HD / 16), chunk = at % (HD / 16);
+      const int key = key0 + row;
+      c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
+      const int block = min(key, n - 1) >> pl.block_shift;
+      c.ks[i] = ks[block], c.vs[i] = vs[block];
+      if (key < n && chunk * 16 < pl.d) {
+        const int64_t from = (int64_t)key * pitch + chunk * 16;
+        c.k[i] = *reinterpret_cast<const uint4*>(kbase + from);
+        c.v[i] = *reinterpret_cast<const uint4*>(vbase + from);
+      }
+    }
+  };
+  auto place = [&](Codes& c, int buf, int t) {
+    const bool partly = (t + 1) * kBlockKeys > all_see;
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < Codes::kPer; i++) {
+      const int at = tid + i * NT, row = at / (HD / 16), chunk = at % (HD / 16);
+      const bool kf = folds(c.ks[i]), vf = folds(c.vs[i]);
+      if (chunk == 0 && (row & 15) == 0) {
+        rest[buf][0][row >> 4] = kf ? 1.f : c.ks[i];
+        rest[buf][1][row >> 4] = vf ? 1.f : c.vs[i];
+      }
+      if (partly) {
+        uint32_t* u = reinterpret_cast<uint32_t*>(&c.v[i]);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const uint32_t is = nan_bytes(u[j]);
+          nan = nan || is != 0;
+          u[j] &= ~(is | (is - (is >> 7)));
+        }
+      }
+      unsigned char* kt = smem + buf * kTile + row * TL::kRowBytes;
+      unsigned char* vt = smem + (2 + buf) * kTile + row * TL::kRowBytes;
+      const float kfold = kf ? c.ks[i] : 1.f, vfold = vf ? c.vs[i] : 1.f;
+      const int sk = TL::swz(row), sv = swz_v<HD>(row);
+      *reinterpret_cast<uint4*>(kt + (((2 * chunk) ^ sk) * 16)) = codes_to_bf16x8(c.k[i].x, c.k[i].y, kfold);
+      *reinterpret_cast<uint4*>(kt + (((2 * chunk + 1) ^ sk) * 16)) = codes_to_bf16x8(c.k[i].z, c.k[i].w, kfold);
+      *reinterpret_cast<uint4*>(vt + (((2 * chunk) ^ sv) * 16)) = codes_to_bf16x8(c.v[i].x, c.v[i].y, vfold);
+      *reinterpret_cast<uint4*>(vt + (((2 * chunk + 1) ^ sv) * 16)) = codes_to_bf16x8(c.v[i].z, c.v[i].w, vfold);
+    }
+    if (partly && nan) nan_seen[buf] = t;
+  };
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int j = 0; j < DB; j++) o[j] = f32x16{0};
+  float m = kNoKey, l = 0.f;  // reference in base 2, this lane's sum
+
+  auto work = [&](int buf, int t) {
+    const unsigned char* ktile = smem + buf * kTile;
+    const unsigned char* vtile = smem + (2 + buf) * kTile;
+    const bool masked = (t + 1) * kBlockKeys > wave_all;
+    float plain = 1.f;  // all ones, or some scale was not folded
+#pragma unroll
+    for (int i = 0; i < 4; i++) plain = rest[buf][0][i] == 1.f && rest[buf][1][i] == 1.f ? plain : 0.f;
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      const int key0 = t * kBlockKeys + 32 * half;
+      bf16x8 kf[KS];
+      read_frags<HD, KS>(kf, ktile, half, l32, hi);
+      f32x16 z = f32x16{0};
+#pragma unroll
+      for (int part = PARTS - 1; part >= 0; part--)
+#pragma unroll
+        for (int j = 0; j < KS; j++) mfma_step(z, kf[j], qf[part][j]);
+      bf16x8 vf[DB][2];
+#pragma unroll
+      for (int j = 0; j < DB; j++)
+#pragma unroll
+        for (int st = 0; st < 2; st++) vf[j][st] = read_vt_frag<HD>(vtile, half, st, j, lane);
+      if (plain == 0.f) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) z[i] *= rest[buf][0][2 * half + (i >> 3)];
+      }
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+          if (key0 + (i >> 2) * 8 + hi * 4 + (i & 3) > last_key) z[i] = -INFINITY;
+      }
+      const float a0 = max3(z[0], z[1], z[2]), a1 = max3(z[3], z[4], z[5]), a2 = max3(z[6], z[7], z[8]);
+      const float a3 = max3(z[9], z[10], z[11]), a4 = max3(z[12], z[13], z[14]);
+      const float top = max_across_halves(max3(max3(a0, a1, a2), max3(a3, a4, z[15]), -INFINITY)) * pl.c2;
+      // the reference follows the maximum lazily, as in the kernel for few rows
+      if (__any(top > m + kLazyBits)) {
+        const float mn = fmaxf(m, top), corr = ex2(m - mn);
+        l *= corr;
+#pragma unroll
+        for (int j = 0; j < DB; j++)
+#pragma unroll
+          for (int i = 0; i < 16; i++) o[j][i] *= corr;
+        m = mn;
+      }
+      float e[16];
+#pragma unroll
+      for (int i = 0; i < 16; i++) e[i] = ex2(fmaf(z[i], pl.c2, -m));
+      l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])) +
+           (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
+      if (plain == 0.f) {
+#pragma unroll
+        for (int i = 0; i < 16; i++) e[i] *= rest[buf][1][2 * half + (i >> 3)];
+      }
+#pragma unroll
+      for (int st = 0; st < 2; st++) {
+        bf16x8 pf[PARTS];
+        weight_frags<PARTS>(pf, e + 8 * st);
+#pragma unroll
+        for (int part = PARTS - 1; part >= 0; part--)
+#pragma unroll
+          for (int j = 0; j < DB; j++) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j][st], pf[part], o[j], 0, 0, 0);
+      }
+    }
+    if (masked && nan_seen[buf] == t) {  // rows that see a NaN code get a NaN in its column
+#pragma unroll 1
+      for (int st = 0; st < 4; st++) {
+        const int key = t * kBlockKeys + 16 * st + 4 * hi;
+        u32x4 u;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          const int at = key + (2 * j & 3) + (j >> 1) * 8;
+          u[j] = (at <= last_key ? 0x3f80u : 0u) | (at + 1 <= last_key ? 0x3f800000u : 0u);
+        }
+#pragma unroll
+        for (int j = 0; j < DB; j++) {
+          const f32x16 seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nan_frag(vbase + min(32 * j + l32, pl.d - 1), pitch, key, n),
+                                                                      __builtin_bit_cast(bf16x8, u), f32x16{0}, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; i++) o[j][i] += seen[i] > 0.f ? NAN : 0.f;
+        }
+      }
+    }
+  };
+
+  {
+    Codes c;
+    if (tid < 2) nan_seen[tid] = -1;
+    __syncthreads();
+    if (first_tile < end_tile) {
+      fetch(c, first_tile);
+      place(c, 0, first_tile);
+      if (first_tile + 1 < end_tile) fetch(c, first_tile + 1);
+    }
+    __syncthreads();
+    for (int t = first_tile; t < end_tile; t++) {
+      const int buf = (t - first_tile) & 1;
+      if (t + 1 < end_tile) {
+        place(c, buf ^ 1, t + 1);
+        if (t + 2 < end_tile) fetch(c, t + 2);
+      }
+      if (active && t * kBlockKeys < wave_any) work(buf, t);
+      __syncthreads();
+    }
+  }
+
+  if (!active || !row_ok) return;
+  const float sum = l + __shfl_xor(l, 32);
+  const bool whole = room.splits == 1, any = sum > 0.f || sum != sum;
+  const float inv = any ? 1.f / sum : 0.f;
+  const size_t orow = ((size_t)b * pl.Hq + h * pl.G + g_row) * pl.p + t_row;
+  const size_t record = (size_t)unit * pl.R + r;
+  if (hi == 0) {
+    if (whole) lse[orow] = any ? (m + log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+    if (whole && room.rows) room.rows[(size_t)bh * pl.R + r] = make_float2(m, inv);
+    if (!whole) room.stats[record] = make_float2(m, sum);
+  }
+#pragma unroll
+  for (int j = 0; j < DB; j++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int column = 32 * j + 8 * i + 4 * hi;
+      if (column >= pl.d) continue;
+      float y[4];
+#pragma unroll
+      for (int x = 0; x < 4; x++) y[x] = !whole ? o[j][4 * i + x] : any ? o[j][4 * i + x] * inv : 0.f;
+      if (whole) store4(out + orow * pl.d + column, y);
+      else store4(room.records + record * pl.d + column, y);
+    }
+}
+
+// What the splits of the rows left, put together: 4 columns to a thread, d / 4 threads to a row.
+template <typename T>
+__global__ __launch_bounds__(256) void kv8_join_rows(Kv8Plan pl, T* __restrict__ out, float* __restrict__ lse, BlockRoom room) {
+  const int per_row = pl.d >> 2;
+  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const size_t row_of_all = at / per_row;
+  if (row_of_all >= (size_t)pl.nb * pl.Hkv * pl.R) return;
+  const int column = (int)(at - row_of_all * per_row) * 4, bh = (int)(row_of_all / pl.R), r = (int)(row_of_all - (size_t)bh * pl.R);
+  const float2* s = room.stats + (size_t)bh * room.splits * pl.R + r;
+  float m = kNoKey, sum = 0.f;
+  for (int i = 0; i < room.splits; i++) m = fmaxf(m, s[(size_t)i * pl.R].x);
+  float y[4] = {0, 0, 0, 0};
+  for (int i = 0; i < room.splits; i++) {
+    const float2 ml = s[(size_t)i * pl.R];
+    const float w = ex2(ml.x - m);
+    sum += ml.y * w;
+    const float4 a = *reinterpret_cast<const float4*>(room.records + (((size_t)bh * room.splits + i) * pl.R + r) * pl.d + column);
+    y[0] += w * a.x, y[1] += w * a.y, y[2] += w * a.z, y[3] += w * a.w;
+  }
+  const bool any = sum > 0.f || sum != sum;
+  const float inv = any ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; i++) y[i] = any ? y[i] * inv : 0.f;
+  const int b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
+  int g, t;
+  head_and_token(pl.p, pl.inv_p, r, g, t);
+  const size_t orow = ((size_t)b * pl.Hq + h * pl.G + g) * pl.p + t;
+  store4(out + orow * pl.d + column, y);
+  if (column == 0) {
+    lse[orow] = any ? (m + log2f(sum)) * 0.69314718055994530942f : -INFINITY;
+    if (room.rows) room.rows[(size_t)bh * pl.R + r] = make_float2(m, inv);
+  }
+}
+
+// weight += the softmax weights of many rows: the product with K once more, now with the keys in registers and the query rows
+// through LDS, so that every key's sum has one owner and one order.  A wave has 32 NK keys.
+template <typename T, int HD, int KS, int NK, int NW>
+__global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_accumulate_block(Kv8Plan pl, const T* __restrict__ q,
+                                                                                               const float2* __restrict__ rows) {
+  using TL = Tile<HD>;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int PARTS = F32 ? 3 : 1, NT = NW * 64, QT = F32 ? 32 : 64;  // query rows of a tile
+  constexpr int kPart = QT * TL::kRowBytes, kTile = PARTS * kPart;
+  constexpr int kPer = QT * TL::kChunks / NT;  // 8-value chunks of a tile per thread
+  static_assert(kPer >= 1, "every thread has a chunk");
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  float4(*info)[QT] = reinterpret_cast<float4(*)[QT]>(smem + 2 * kTile);  // reference, 1 / sum, last key
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hi = lane >> 5;
+  const int bh = blockIdx.y, b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
+  const int old = kv8_old_rows(pl, bh), n = old + pl.n_block;
+  const int first_key = blockIdx.x * (32 * NK * NW), key0 = first_key + wave * 32 * NK;
+  if (first_key >= n) return;
+  const uint8_t* kbase = pl.k + b * pl.sb + h * pl.sh;
+  const float* ks = pl.k_scale + b * pl.ssb + h * pl.ssh;
+
+  bf16x8 kf[NK][KS];
+  float rest[NK][2];
+#pragma unroll
+  for (int x = 0; x < NK; x++) {
+    const int key = min(key0 + 32 * x + l32, n - 1);
+    const float scale = ks[key >> pl.block_shift];
+    const float fold = folds(scale) ? scale : 1.f;
+#pragma unroll
+    for (int s = 0; s < 2; s++) {
+      const float of16 = ks[min(key0 + 32 * x + 16 * s, n - 1) >> pl.block_shift];
+      rest[x][s] = folds(of16) ? 1.f : of16;
+    }
+    const uint8_t* row = kbase + (int64_t)key * pl.st;
+#pragma unroll
+    for (int j = 0; j < KS; j++) {
+      const int at = (2 * j + hi) * 8;
+      uint2 u = make_uint2(0, 0);
+      if (at < pl.d) u = *reinterpret_cast<const uint2*>(row + at);
+      kf[x][j] = __builtin_bit_cast(bf16x8, codes_to_bf16x8(u.x, u.y, fold));
+    }
+  }
+  float acc[NK][16];
+#pragma unroll
+  for (int x = 0; x < NK; x++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) acc[x][i] = 0.f;
+
+  struct Share {
+    float v[kPer][8];
+    float4 info;
+  };
+  auto fetch = [&](Share& c, int tile) {
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+      const int at = tid + i * NT, r = tile * QT + at / TL::kChunks, column = at % TL::kChunks * 8;
+      int g, t;
+      head_and_token(pl.p, pl.inv_p, min(r, pl.R - 1), g, t);
+      const T* from = q + b * pl.qsb + (int64_t)(h * pl.G + g) * pl.qsh + (int64_t)t * pl.qst + column;
+      float4 a = make_float4(0, 0, 0, 0), z = a;
+      if (column < pl.d && r < pl.R) {  // no row: zeros, not what the last one holds, which may be NaN
+        a = reinterpret_cast<const float4*>(from)[0];
+        if (F32) z = reinterpret_cast<const float4*>(from)[1];
+      }
+      c.v[i][0] = a.x, c.v[i][1] = a.y, c.v[i][2] = a.z, c.v[i][3] = a.w;
+      if (F32) c.v[i][4] = z.x, c.v[i][5] = z.y, c.v[i][6] = z.z, c.v[i][7] = z.w;
+    }
+    if (tid < QT) {
+      const int r = tile * QT + tid;
+      float2 ml = make_float2(0.f, 0.f);
+      int g = 0, t = 0;
+      if (r < pl.R) {
+        ml = rows[(size_t)bh * pl.R + r];
+        head_and_token(pl.p, pl.inv_p, r, g, t);
+      }
+      // a row without weights: whatever its logits, exponentials of -inf
+      c.info = make_float4(ml.y == 0.f ? INFINITY : ml.x, ml.y, __int_as_float(pl.causal ? old + t : n - 1), 0.f);
+    }
+  };
+  auto place = [&](Share& c, int buf) {
+    unsigned char* tile = smem + buf * kTile;
+#pragma unroll
+    for (int i = 0; i < kPer; i++) {
+      const int at = tid + i * NT, r = at / TL::kChunks, chunk = at % TL::kChunks;
+      uint4* to = reinterpret_cast<uint4*>(tile + r * TL::kRowBytes + ((chunk ^ TL::swz(r)) * 16));
+      if constexpr (F32) {
+        bf16x8 parts[3];
+        cut_row8(parts, c.v[i], true);
+#pragma unroll
+        for (int p = 0; p < 3; p++) *(to + p * (kPart / 16)) = __builtin_bit_cast(uint4, parts[p]);
+      } else {
+        *to = make_uint4(__float_as_uint(c.v[i][0]), __float_as_uint(c.v[i][1]), __float_as_uint(c.v[i][2]), __float_as_uint(c.v[i][3]));
+      }
+    }
+    if (tid < QT) info[buf][tid] = c.info;
+  };
+
+  const int tiles = (pl.R + QT - 1) / QT;
+  Share c;
+  fetch(c, 0);
+  place(c, 0);
+  if (tiles > 1) fetch(c, 1);
+  __syncthreads();
+  for (int t = 0; t < tiles; t++) {
+    const int buf = t & 1;
+    if (t + 1 < tiles) {
+      place(c, buf ^ 1);
+      if (t + 2 < tiles) fetch(c, t + 2);
+    }
+#pragma unroll
+    for (int half = 0; half < QT / 32; half++) {
+      int least, most;
+      const int row0 = t * QT + 32 * half;
+      rows_see(pl, old, n, row0, row0 + 32, least, most);
+      if (row0 >= pl.R || key0 >= most) continue;
+      bf16x8 qf[PARTS][KS];
+#pragma unroll
+      for (int p = 0; p < PARTS; p++) read_frags<HD, KS>(qf[p], smem + buf * kTile + p * kPart, half, l32, hi);
+      const float4 row = info[buf][32 * half + l32];
+      const int last = __float_as_int(row.z);
+#pragma unroll
+      for (int x = 0; x < NK; x++) {
+        f32x16 z = f32x16{0};
+#pragma unroll
+        for (int p = PARTS - 1; p >= 0; p--)
+#pragma unroll
+          for (int j = 0; j < KS; j++) mfma_step(z, kf[x][j], qf[p][j]);
+        if (rest[x][0] != 1.f || rest[x][1] != 1.f) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) z[i] *= rest[x][i >> 3];
+        }
+        const bool masked = key0 + 32 * x + 32 > least;
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 16; i++) {
+            const bool seen = key0 + 32 * x + (i >> 2) * 8 + hi * 4 + (i & 3) <= last;
+            acc[x][i] += seen ? ex2(fmaf(z[i], pl.c2, -row.x)) * row.y : 0.f;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; i++) acc[x][i] = fmaf(ex2(fmaf(z[i], pl.c2, -row.x)), row.y, acc[x][i]);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  float* weight = pl.weight + b * pl.rsb + h * pl.rsh;
+#pragma unroll
+  for (int x = 0; x < NK; x++)
+#pragma unroll
+    for (int i = 0; i < 16; i++) {
+      float s = acc[x][i];
+#pragma unroll
+      for (int lanes = 1; lanes < 32; lanes <<= 1) s += __shfl_xor(s, lanes);
+      const int key = key0 + 32 * x + (i >> 2) * 8 + hi * 4 + (i & 3);
+      if (l32 == 0 && key < n) weight[key] += s;
+    }
+}
+
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Room of the kernel for few rows; null workspace: only its size, in *bytes.
@@ -652,26 +1054,93 @@ hipError_t launch_tokens(const Kv8Plan& pl, const T* q, T* out, float* lse, void
   return hipGetLastError();
 }
 
+BlockRoom block_room(const Kv8Plan& pl, void* workspace, size_t* bytes) {
+  const int64_t heads = (int64_t)pl.nb * pl.Hkv;
+  const int nw = block_waves(pl), n_rb = (pl.R + 32 * nw - 1) / (32 * nw);
+  const int tiles = (pl.n_cached + pl.n_block + kBlockKeys - 1) / kBlockKeys;
+  const int64_t slots = kComputeUnits * (nw == 2 ? 2 : 1) * block_occupancy(pl.dtype == EPICACHE_DTYPE_F32 ? 4 : 2, pl.d <= 128 ? 128 : 256);
+  int64_t splits = slots / (heads * n_rb);  // a round of workgroups, each with four tiles at least
+  splits = std::max<int64_t>(1, std::min<int64_t>({splits, tiles / 4, kMostSplits}));
+  const int split_tiles = (tiles + (int)splits - 1) / (int)splits;
+  splits = (tiles + split_tiles - 1) / split_tiles;
+  BlockRoom room = {(int)splits, split_tiles, nullptr, nullptr, nullptr};
+  char* ws = static_cast<char*>(workspace);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    char* p = ws ? ws + at : nullptr;
+    at += align256(n);
+    return reinterpret_cast<float*>(p);
+  };
+  if (pl.accumulate) room.rows = reinterpret_cast<float2*>(take((size_t)heads * pl.R * sizeof(float2)));
+  if (splits > 1) {
+    room.stats = reinterpret_cast<float2*>(take((size_t)heads * splits * pl.R * sizeof(float2)));
+    room.records = take((size_t)heads * splits * pl.R * pl.d * sizeof(float));
+  }
+  *bytes = at;
+  return room;
+}
+
+template <typename K, typename... A>
+hipError_t launch_with_lds(K kernel, dim3 grid, int threads, size_t lds, hipStream_t stream, A... args) {
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, stream, args...);
+  return hipGetLastError();
+}
+
+template <typename T, int HD, int KS, int DB, int NW>
+hipError_t launch_block(const Kv8Plan& pl, const T* q, T* out, float* lse, void* workspace, hipStream_t stream) {
+  size_t bytes;
+  const BlockRoom room = block_room(pl, workspace, &bytes);
+  const int heads = pl.nb * pl.Hkv, n_rb = (pl.R + 32 * NW - 1) / (32 * NW);
+  hipError_t e = launch_with_lds(kv8_attention_block<T, HD, KS, DB, NW>, dim3(8 * n_rb, (heads * room.splits + 7) / 8), NW * 64,
+                                 4 * kBlockKeys * Tile<HD>::kRowBytes + 128, stream, pl, q, out, lse, room);
+  if (e != hipSuccess) return e;
+  if (room.splits > 1) {
+    const size_t threads = (size_t)heads * pl.R * (pl.d / 4);
+    hipLaunchKernelGGL(kv8_join_rows<T>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, pl, out, lse, room);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!pl.accumulate) return hipSuccess;
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = sizeof(T) == 4 ? 32 : 64, NK = HD == 256 ? 1 : 2;
+  constexpr size_t lds = 2 * PARTS * QT * Tile<HD>::kRowBytes + 2 * QT * sizeof(float4);
+  const int keys = 32 * NK * 4;
+  return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + keys - 1) / keys, heads), 256, lds,
+                         stream, pl, q, room.rows);
+}
+
+template <typename T>
+hipError_t launch_blocks(const Kv8Plan& pl, const T* q, T* out, float* lse, void* workspace, hipStream_t stream) {
+  auto waves = [&](auto hd, auto ks, auto db) {
+    constexpr int HD = decltype(hd)::value, KS = decltype(ks)::value, DB = decltype(db)::value;
+    if (block_waves(pl) == 2) return launch_block<T, HD, KS, DB, 2>(pl, q, out, lse, workspace, stream);
+    return launch_block<T, HD, KS, DB, 4>(pl, q, out, lse, workspace, stream);
+  };
+  using std::integral_constant;
+  if (pl.d <= 64) return waves(integral_constant<int, 64>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  if (pl.d <= 128) return waves(integral_constant<int, 128>{}, integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  if (pl.d <= 192) return waves(integral_constant<int, 256>{}, integral_constant<int, 12>{}, integral_constant<int, 6>{});
+  return waves(integral_constant<int, 256>{}, integral_constant<int, 16>{}, integral_constant<int, 8>{});
+}
+
 }  // namespace
 
 size_t kv8_attention_workspace(const Kv8Plan& pl) {
-  if (few_rows(pl)) {
-    size_t bytes;
-    token_room(pl, nullptr, &bytes);
-    return bytes;
-  }
-  return pl.accumulate ? (size_t)pl.nb * pl.Hq * pl.p * sizeof(float2) : 0;
+  size_t bytes;
+  if (few_rows(pl)) token_room(pl, nullptr, &bytes);
+  else block_room(pl, nullptr, &bytes);
+  return bytes;
 }
 
 hipError_t launch_kv8_attention(const Kv8Plan& pl, const void* q, void* out, float* lse, void* workspace, hipStream_t stream) {
-  if (few_rows(pl)) {
-    if (pl.dtype == EPICACHE_DTYPE_BF16)
-      return launch_tokens(pl, static_cast<const __hip_bfloat16*>(q), static_cast<__hip_bfloat16*>(out), lse, workspace, stream);
-    return launch_tokens(pl, static_cast<const float*>(q), static_cast<float*>(out), lse, workspace, stream);
-  }
-  float2* stats = pl.accumulate ? static_cast<float2*>(workspace) : nullptr;
-  return pl.dtype == EPICACHE_DTYPE_BF16 ? launch<__hip_bfloat16>(pl, q, out, lse, stats, stream)
-                                         : launch<float>(pl, q, out, lse, stats, stream);
+  auto typed = [&](auto* rows, auto* to) {
+    return few_rows(pl) ? launch_tokens(pl, rows, to, lse, workspace, stream) : launch_blocks(pl, rows, to, lse, workspace, stream);
+  };
+  if (pl.dtype == EPICACHE_DTYPE_BF16) return typed(static_cast<const __hip_bfloat16*>(q), static_cast<__hip_bfloat16*>(out));
+  return typed(static_cast<const float*>(q), static_cast<float*>(out));
 }
 
 }  // namespace epicache

@@ -34,16 +34,7 @@
 namespace epicache {
 namespace {
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-
 constexpr float kLazyBits = 8.f;
-
-// V tiles use their own swizzle: 16-byte chunk c of key row r sits at position c ^ swz_v(r), so the four
-// key rows that one transposing load touches fall into different 64-byte bank groups.
-template <int HD>
-__device__ __forceinline__ int swz_v(int r) { return HD == 64 ? 4 * (r & 1) : 4 * (r & 3); }
 
 // Staging of one TK-row tile by NW waves, 1 KiB slabs; wave w takes slabs w, w + NW, ..  Full tiles go through a
 // uniform slab address and a lane offset that only depends on the slab through the swizzle.
@@ -91,56 +82,6 @@ struct TileStager {
   }
 };
 
-// A operand of O^T += V^T P^T for head_dim block `dblk` (32 columns) and the 16-key step `kstep` of the
-// 32-key half `ks`: lane (m = l % 32, hi = l / 32) needs keys {4 hi .. 4 hi + 3} and {8 + 4 hi .. 8 + 4 hi + 3}
-// (+ 16 kstep + 32 ks) of column 32 dblk + m, the key order in which the softmax weights sit in the lane.
-template <int HD>
-__device__ __forceinline__ bf16x8 read_vt_frag(const unsigned char* vtile, int ks, int kstep, int dblk, int lane) {
-  const int s = lane & 15, gh = (lane >> 4) & 1, hi = lane >> 5;
-  const int chunk = 4 * dblk + 2 * gh + ((s & 3) >> 1);      // 16-byte chunk of the row this lane points into
-  const int half = (s & 1) * 8;
-  s16x4 part[2];
-#pragma unroll
-  for (int g = 0; g < 2; g++) {
-    const int row = 32 * ks + 16 * kstep + 8 * g + 4 * hi + (s >> 2);
-    const unsigned char* p = vtile + row * Tile<HD>::kRowBytes + ((chunk ^ swz_v<HD>(row)) * 16) + half;
-    part[g] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)LDS_PTR(p));
-  }
-  typedef __attribute__((ext_vector_type(8))) short s16x8;
-  const s16x8 both = {part[0][0], part[0][1], part[0][2], part[0][3], part[1][0], part[1][1], part[1][2], part[1][3]};
-  return __builtin_bit_cast(bf16x8, both);
-}
-
-// Eight fp32 weights as PARTS bf16 operands: rounded to one, or cut into three (8 + 8 + 8 bits of the significand)
-// whose sum is exact.
-template <int PARTS>
-__device__ __forceinline__ void weight_frags(bf16x8 (&p)[PARTS], const float* e) {
-  typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-  if constexpr (PARTS == 1) {
-    u32x4 packed;
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const f32x2 pair = {e[2 * j], e[2 * j + 1]};
-      packed[j] = __builtin_bit_cast(unsigned int, __builtin_convertvector(pair, bf16x2));
-    }
-    p[0] = __builtin_bit_cast(bf16x8, packed);
-  } else {
-    u32x4 packed[PARTS];
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-      float a = e[2 * j], b = e[2 * j + 1];
-#pragma unroll
-      for (int i = 0; i < PARTS; i++) {
-        const unsigned int ua = __float_as_uint(a), ub = __float_as_uint(b);
-        packed[i][j] = __builtin_amdgcn_perm(ub, ua, 0x07060302);  // the upper halves, b's above a's
-        a -= __uint_as_float(ua & 0xffff0000u), b -= __uint_as_float(ub & 0xffff0000u);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < PARTS; i++) p[i] = __builtin_bit_cast(bf16x8, packed[i]);
-  }
-}
-
 // What the infinities and NaNs among the values add to one 32 x 32 block of O^T, for 16 keys: v as read from V, keys
 // key + 0 .. 3 and key + 8 .. 11, of which the lane's row sees those up to last_key, w their weights.  Whether a row sees
 // one of a kind is a product of zeros and ones.
@@ -171,14 +112,6 @@ __device__ __forceinline__ void add_not_finite(f32x16& o, bf16x8& v, int key, in
   for (int j = 0; j < 8; j++)
     if ((bits[j] & 0x7f80) == 0x7f80) bits[j] = 0;
   v = __builtin_bit_cast(bf16x8, bits);
-}
-
-// max(x[l], x[l ^ 32]) in every lane, on the vector ALU: the swap leaves the lower half's values in both
-// halves of one register and the upper half's in both halves of the other.
-__device__ __forceinline__ float max_across_halves(float x) {
-  const unsigned int u = __float_as_uint(x);
-  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // The row maximum is taken with compiler-visible max operations, not the hand-written v_max3_f32 of the scoring
