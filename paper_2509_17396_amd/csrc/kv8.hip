@@ -138,151 +138,368 @@ __device__ __forceinline__ uint32_t evict_key(float weight, int position, int la
   return max(min(order_key(weight), 0xff800001u), 1u);
 }
 
-// Which rows stay, and which row takes the place of one that goes.  One workgroup per head; the keys are made again in every sweep.
-// Leaves row_from, n_kept, the moved rows' weight and position, and the scales of the block that K cuts (blocks below it
-// take rows of it, and it takes rows itself).
-__global__ __launch_bounds__(1024) void kv8_choose(Kv8Plan pl, const int32_t* __restrict__ budgets, int32_t* n_kept,
-                                                   int32_t* row_from, int pitch, int32_t* sources, float2* cut_scales) {
-  __shared__ uint32_t hist_rep[256 * kHistCopies];
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t wave_a[16], wave_b[16];
-  __shared__ int wave_latest[16];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+// The largest magnitude among 16 codes that are numbers, as a code, and whether there are others.
+__device__ __forceinline__ uint32_t largest_code(uint4 u) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+  u16x2 most = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    uint32_t x = w[i] & 0x7f7f7f7fu;
+    const uint32_t nan = (x + 0x01010101u) & 0x80808080u;
+    x &= ~(nan | (nan - (nan >> 7)));
+    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x & 0x00ff00ffu));
+    most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, (x >> 8) & 0x00ff00ffu));
+  }
+  return most[0] > most[1] ? most[0] : most[1];
+}
+__device__ __forceinline__ float code_value(uint32_t code) {
+  float x[4];
+  decode4(code, x);
+  return x[0];
+}
+
+// What a head's eviction leaves for its moves: row holes[j] gets what row sources[j] holds; starts[i]: the moves into blocks before
+// block i.
+struct Moves {
+  int32_t* holes;    // [heads][pitch]
+  int32_t* sources;  // [heads][pitch]
+  int32_t* starts;   // [heads][blocks + 1]
+  float2* cut;       // [heads]: the scales of the block that K cuts, as they were
+  int pitch, blocks;
+};
+
+// By one wave: the moves first .. end - 1 of head (b, h), all into block `block`, of K and V and of the rows' weight and position.
+// K: rows that stay in the cache.  The block that K cuts may both take and give rows, so its scales as they were come from the caller.
+__device__ __forceinline__ void move_block(const Kv8Plan& pl, int b, int h, const int32_t* holes, const int32_t* sources, int first,
+                                           int end, int block, int K, float2 cut_scale, int lane) {
+  constexpr int kHeld = 2;  // chunks of 16 codes of K and of V per lane that stay in registers between the two looks at them
+  const int d = pl.d, shift = pl.block_shift;
+  const int64_t pitch = pl.st;
+  uint8_t* const codes[2] = {pl.k + b * pl.sb + h * pl.sh, pl.v + b * pl.sb + h * pl.sh};
+  float* const scale[2] = {pl.k_scale + b * pl.ssb + h * pl.ssh, pl.v_scale + b * pl.ssb + h * pl.ssh};
+  const int per_row = d >> 4, chunks = (end - first) * per_row, cut = K >> shift;
+  const float inv = 1.f / (float)per_row;
+  const int here = min(1 << shift, K - (block << shift));
+  const bool any_stays = end - first < here;
+  const float was[2] = {block == cut ? cut_scale.x : scale[0][block], block == cut ? cut_scale.y : scale[1][block]};
+  struct Look {
+    uint4 u[2];
+    float s[2];
+    int64_t to;
+  };
+  auto look = [&](int at, Look& x) {
+    const int row = (int)(((float)at + 0.5f) * inv);  // at / per_row: at < 2048, per_row <= 16
+    const int from = sources[first + row], column = (at - row * per_row) * 16, block_of = from >> shift;
+    x.to = (int64_t)holes[first + row] * pitch + column;
+#pragma unroll
+    for (int v = 0; v < 2; v++) {
+      x.u[v] = *reinterpret_cast<const uint4*>(codes[v] + (int64_t)from * pitch + column);
+      x.s[v] = scale[v][block_of];
+    }
+    if (block_of == cut) x.s[0] = cut_scale.x, x.s[1] = cut_scale.y;
+  };
+  Look held[kHeld];
+  float amax[2] = {0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < kHeld; c++)
+    if (lane + c * 64 < chunks) look(lane + c * 64, held[c]);
+  for (int j = first + lane; j < end; j += 64) {  // rows from K on are not written, so what is read here is what was there
+    const int64_t of = b * pl.rsb + h * pl.rsh;
+    const int to = holes[j], from = sources[j];
+    pl.weight[of + to] = pl.weight[of + from];
+    if (pl.position) pl.position[of + to] = pl.position[of + from];
+  }
+#pragma unroll
+  for (int c = 0; c < kHeld; c++)
+    if (lane + c * 64 < chunks) {
+#pragma unroll
+      for (int v = 0; v < 2; v++) amax[v] = fmaxf(amax[v], code_value(largest_code(held[c].u[v])) * held[c].s[v]);
+    }
+  for (int at = lane + kHeld * 64; at < chunks; at += 64) {
+    Look x;
+    look(at, x);
+#pragma unroll
+    for (int v = 0; v < 2; v++) amax[v] = fmaxf(amax[v], code_value(largest_code(x.u[v])) * x.s[v]);
+  }
+  float now[2];
+#pragma unroll
+  for (int v = 0; v < 2; v++) {
+    amax[v] = __uint_as_float(wave_reduce(__float_as_uint(amax[v]), [](uint32_t x, uint32_t y) { return x > y ? x : y; }));
+    now[v] = scale_for(amax[v]);
+    if (any_stays) now[v] = fmaxf(now[v], was[v]);
+  }
+  auto again = [&](uint4 u, float from, float to) {
+    if (from == to) return u;
+    float x[16];
+    decode16(u, x, from);
+    return encode16(x, to);
+  };
+  auto put = [&](const Look& x) {
+#pragma unroll
+    for (int v = 0; v < 2; v++) *reinterpret_cast<uint4*>(codes[v] + x.to) = again(x.u[v], x.s[v], now[v]);
+  };
+#pragma unroll
+  for (int c = 0; c < kHeld; c++)
+    if (lane + c * 64 < chunks) put(held[c]);
+  for (int at = lane + kHeld * 64; at < chunks; at += 64) {
+    Look x;
+    look(at, x);
+    put(x);
+  }
+#pragma unroll
+  for (int v = 0; v < 2; v++) {  // the rows that stay, where their scale has grown
+    if (!(any_stays && now[v] > was[v])) continue;
+    for (int at = lane; at < here * per_row; at += 64) {
+      const int row = (int)(((float)at + 0.5f) * inv), i = (block << shift) + row;
+      bool moved = false;
+      for (int j = first; j < end; j++) moved = moved || holes[j] == i;
+      uint4* p = reinterpret_cast<uint4*>(codes[v] + (int64_t)i * pitch + (at - row * per_row) * 16);
+      if (!moved) *p = again(*p, was[v], now[v]);
+    }
+  }
+  if (lane == 0) scale[0][block] = now[0], scale[1][block] = now[1];
+}
+
+// Which rows stay, and which row takes the place of one that goes.  One workgroup of NW waves per head; VPT keys per thread in
+// registers, or (VPT = 0) made again in every sweep where the rows are too many.
+// Leaves the moves and n_kept.  FUSED: makes the moves as well, a wave per block, and row_from_opt; the lists stay in LDS if they fit.
+template <int VPT, int NW, bool FUSED>
+__global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t* __restrict__ budgets, int32_t* n_kept,
+                                                      int32_t* row_from_opt, Moves mv) {
+  constexpr bool kHeld = VPT > 0;
+  constexpr int kRegs = kHeld ? VPT : 4;
+  __shared__ SelectLds<NW> sm;
+  __shared__ uint32_t hist_rep[kHeld ? 1 : 256 * kHistCopies];
+  __shared__ uint32_t hist[kHeld ? 1 : 256];
+  __shared__ uint32_t wave_a[NW], wave_b[NW];
+  __shared__ int wave_latest[NW];
+  __shared__ int32_t near_holes[FUSED ? 64 : 1], near_sources[FUSED ? 64 : 1];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.x, b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
-  const int n = kv8_old_rows(pl, bh) + pl.n_block;
+  const int n = kv8_old_rows(pl, bh) + pl.n_block, shift = pl.block_shift;
   int M = pl.budget;
   if (budgets) M = max(0, min(M, budgets[b]));
   const int K = min(M, n);
   float* weight = pl.weight + b * pl.rsb + h * pl.rsh;
   int32_t* position = pl.position ? pl.position + b * pl.rsb + h * pl.rsh : nullptr;
-  int32_t* out = row_from + (size_t)bh * pitch;
-  int32_t* src = sources + (size_t)bh * pitch;
-  if (tid == 0) {
-    const int64_t cut = b * pl.ssb + h * pl.ssh + (K >> pl.block_shift);
-    cut_scales[bh] = K < n ? make_float2(pl.k_scale[cut], pl.v_scale[cut]) : make_float2(0.f, 0.f);
-  }
+  float* k_scale = pl.k_scale + b * pl.ssb + h * pl.ssh;
+  float* v_scale = pl.v_scale + b * pl.ssb + h * pl.ssh;
+  int32_t* out = FUSED && row_from_opt ? row_from_opt + (size_t)bh * mv.pitch : nullptr;
+  int32_t* holes_of = mv.holes + (size_t)bh * mv.pitch;
+  int32_t* sources_of = mv.sources + (size_t)bh * mv.pitch;
+  int32_t* starts = mv.starts + (size_t)bh * (mv.blocks + 1);
+  const int kept_blocks = (K + (1 << shift) - 1) >> shift;
   if (K == n || K == 0) {  // all stay, or none
-    for (int i = tid; i < pitch; i += 1024) out[i] = i < K ? i : -1;
+    if (out)
+      for (int i = tid; i < mv.pitch; i += NW * 64) out[i] = i < K ? i : -1;
+    for (int i = tid; i <= mv.blocks; i += NW * 64) starts[i] = 0;
     if (tid == 0) n_kept[bh] = K;
     return;
   }
-  int latest = INT32_MIN;
-  for (int i = tid; i < n; i += 1024) latest = max(latest, position ? position[i] : i);
-  latest = (int)(wave_reduce((uint32_t)latest ^ 0x80000000u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }) ^ 0x80000000u);
-  if (lane == 0) wave_latest[wave] = latest;
-  for (int i = tid; i < 256 * kHistCopies; i += 1024) hist_rep[i] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 16; w++) latest = max(latest, wave_latest[w]);
+  const float2 cut = make_float2(k_scale[K >> shift], v_scale[K >> shift]);
+  if (tid == 0) mv.cut[bh] = cut;
 
-  const int groups = (n + 1023) / 1024;  // 64-wide groups per wave
+  const int groups = kHeld ? VPT : (n + NW * 64 - 1) / (NW * 64);  // 64-wide groups per wave
   const int base = wave * groups * 64 + lane;
-  auto key_at = [&](int i) -> uint32_t { return i < n ? evict_key(weight[i], position ? position[i] : i, latest, pl.n_recent) : 0u; };
-
-  uint32_t prefix = 0, mask = 0, kth = (uint32_t)K;
-#pragma unroll 1
-  for (int pass = 0; pass < 4; pass++) {
-    const int shift = 24 - 8 * pass;
-    for (int j = 0; j < groups; j++) {
-      const uint32_t key = key_at(base + j * 64);
-      if (key != 0 && (key & mask) == prefix) hist_count(hist_rep, (key >> shift) & 255u, lane);
+  const bool by_position = pl.n_recent > 0 && position != nullptr;
+  int latest = n - 1;
+  float w[kRegs];
+  int pos[kRegs];
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int j = 0; j < kRegs; j++) w[j] = weight[min(base + j * 64, n - 1)];
+    if (by_position) {
+#pragma unroll
+      for (int j = 0; j < kRegs; j++) pos[j] = position[min(base + j * 64, n - 1)];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kRegs; j++) pos[j] = base + j * 64;
     }
-    __syncthreads();
-    hist_fold(hist_rep, hist, tid);
-    __syncthreads();
-    uint32_t bin, above;
-    locate_digit(hist, kth, lane, bin, above);
-    prefix |= bin << shift;
-    mask |= 255u << shift;
-    kth -= above;
   }
-  const uint32_t thr = prefix, need_eq = kth;
+  if (by_position) {
+    latest = INT32_MIN;
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int j = 0; j < kRegs; j++) latest = max(latest, pos[j]);
+    } else {
+      for (int i = tid; i < n; i += NW * 64) latest = max(latest, position[i]);
+    }
+    latest = (int)(wave_reduce((uint32_t)latest ^ 0x80000000u, [](uint32_t x, uint32_t y) { return x > y ? x : y; }) ^ 0x80000000u);
+    if (lane == 0) wave_latest[wave] = latest;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NW; x++) latest = max(latest, wave_latest[x]);
+  }
+  auto key_at = [&](int i) -> uint32_t {
+    return i < n ? evict_key(weight[i], by_position ? position[i] : i, latest, pl.n_recent) : 0u;
+  };
 
-  // ties before this wave
-  uint32_t ceq = 0;
-  for (int j = 0; j < groups; j++) ceq += __popcll(__ballot(key_at(base + j * 64) == thr));
-  if (lane == 0) wave_a[wave] = ceq;
-  __syncthreads();
-  uint32_t eq_first = 0;
-  for (int w = 0; w < wave; w++) eq_first += wave_a[w];
-  auto each = [&](auto f) {
-    uint32_t eq = eq_first;
-    for (int j = 0; j < groups; j++) {
-      const int i = base + j * 64;
-      const uint32_t key = key_at(i);
-      const uint64_t beq = __ballot(key == thr);
-      f(i, key > thr || (key == thr && eq + lanes_below(beq) < need_eq));
-      eq += __popcll(beq);
+  uint32_t keys[kRegs];
+  uint32_t thr, need_eq;
+  bool cut_ties = true;
+  if constexpr (kHeld) {
+    uint32_t least = 0xffffffffu;
+#pragma unroll
+    for (int j = 0; j < kRegs; j++) {
+      const uint32_t key = evict_key(w[j], pos[j], latest, pl.n_recent);
+      keys[j] = base + j * 64 < n ? key : 0u;
+      if (base + j * 64 < n) least = min(least, key);
+    }
+    const Threshold t = select_threshold<kRegs, NW>(keys, least, n, (uint32_t)K, wave, lane, sm);
+    thr = t.thr, need_eq = t.need_eq, cut_ties = t.cut;
+  } else {
+    for (int i = tid; i < 256 * kHistCopies; i += NW * 64) hist_rep[i] = 0;
+    __syncthreads();
+    uint32_t prefix = 0, mask = 0, kth = (uint32_t)K;
+#pragma unroll 1
+    for (int pass = 0; pass < 4; pass++) {
+      const int digit = 24 - 8 * pass;
+      for (int j = 0; j < groups; j++) {
+        const uint32_t key = key_at(base + j * 64);
+        if (key != 0 && (key & mask) == prefix) hist_count(hist_rep, (key >> digit) & 255u, lane);
+      }
+      __syncthreads();
+      hist_fold(hist_rep, hist, tid);
+      __syncthreads();
+      uint32_t bin, above;
+      locate_digit(hist, kth, lane, bin, above);
+      prefix |= bin << digit;
+      mask |= 255u << digit;
+      kth -= above;
+    }
+    thr = prefix, need_eq = kth;
+  }
+  auto each_key = [&](auto f) {
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int j = 0; j < kRegs; j++) {
+        one_group_at_a_time();
+        f(base + j * 64, keys[j]);
+      }
+    } else {
+      for (int j = 0; j < groups; j++) f(base + j * 64, key_at(base + j * 64));
     }
   };
-  __syncthreads();  // wave_a has been read
-  uint32_t holes = 0, from = 0;
-  each([&](int i, bool kept) {
-    holes += __popcll(__ballot(i < K && !kept));
-    from += __popcll(__ballot(i >= K && kept));
-  });
-  if (lane == 0) wave_a[wave] = holes, wave_b[wave] = from;
-  __syncthreads();
-  holes = 0, from = 0;
-  for (int w = 0; w < wave; w++) holes += wave_a[w], from += wave_b[w];
-  each([&](int i, bool kept) {
-    const uint64_t m = __ballot(i >= K && kept);
-    if (i >= K && kept) src[from + lanes_below(m)] = i;
-    from += __popcll(m);
-  });
-  __threadfence_block();
-  __syncthreads();
-  // weight and position below K change only in the places that are looked at no more
-  each([&](int i, bool kept) {
-    const bool hole = i < K && !kept;
-    const uint64_t m = __ballot(hole);
-    if (i < K) out[i] = hole ? src[holes + lanes_below(m)] : i;
-    holes += __popcll(m);
-  });
-  __threadfence_block();
-  __syncthreads();
-  for (int i = tid; i < pitch; i += 1024) {
-    if (i >= K) {
-      out[i] = -1;
-      continue;
-    }
-    const int f = out[i];
-    if (f == i) continue;
-    weight[i] = weight[f];
-    if (position) position[i] = position[f];
+  thr = __builtin_amdgcn_readfirstlane(thr);
+  uint32_t eq_first = 0;  // ties before this wave, where not all of them stay
+  if (cut_ties) {
+    uint32_t ceq = 0;
+    each_key([&](int, uint32_t key) { ceq += __popcll(__ballot(key == thr)); });
+    if (lane == 0) wave_a[wave] = ceq;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NW; x++) eq_first += x < wave ? wave_a[x] : 0;
+    __syncthreads();  // wave_a has been read
   }
+  // f(row, stays): holes are rows below K that go, sources rows from K on that stay
+  auto each_row = [&](auto f) {
+    uint32_t eq = eq_first, t = thr;
+    asm volatile("" : "+s"(t));  // the masks are made again, not kept in scalar registers from one sweep to the next
+    if (cut_ties) {
+      each_key([&](int i, uint32_t key) {
+        const uint64_t beq = __ballot(key == t);
+        f(i, key > t || (key == t && eq + lanes_below(beq) < need_eq));
+        eq += __popcll(beq);
+      });
+    } else {
+      each_key([&](int i, uint32_t key) { f(i, key >= t); });
+    }
+  };
+  uint32_t holes = 0, sources = 0;
+  each_row([&](int i, bool stays) {
+    holes += i < K && !stays;
+    sources += i >= K && stays;
+  });
+  auto add = [](uint32_t x, uint32_t y) { return x + y; };
+  holes = wave_reduce(holes, add), sources = wave_reduce(sources, add);
+  if (lane == 0) wave_a[wave] = holes, wave_b[wave] = sources;
+  __syncthreads();
+  holes = 0, sources = 0;
+  uint32_t moves = 0;
+#pragma unroll
+  for (int x = 0; x < NW; x++) {
+    if (x < wave) holes += wave_a[x], sources += wave_b[x];
+    moves += wave_a[x];
+  }
+  const uint32_t holes_first = holes;
+  const bool near = FUSED && moves <= 64;
+  if (near) holes_of = near_holes, sources_of = near_sources;
+  each_row([&](int i, bool stays) {
+    const int first = i - lane;  // rows first .. first + 63 here: all on one side of K, but for the ones around it
+    if (first < K) {
+      const bool hole = i < K && !stays;
+      const uint64_t mask = __ballot(hole);
+      const uint32_t before = holes + lanes_below(mask);
+      if (hole) holes_of[before] = i;
+      if (!near && i < K && (i & ((1 << shift) - 1)) == 0) starts[i >> shift] = (int32_t)before;
+      holes += __popcll(mask);
+    }
+    if (first + 64 > K) {
+      const bool source = i >= K && stays;
+      const uint64_t mask = __ballot(source);
+      if (source) sources_of[sources + lanes_below(mask)] = i;
+      sources += __popcll(mask);
+    }
+  });
+  if (!near)
+    for (int i = kept_blocks + tid; i <= mv.blocks; i += NW * 64) starts[i] = (int32_t)moves;
   if (tid == 0) n_kept[bh] = K;
+  if constexpr (FUSED) {
+    if (!near) __threadfence_block();
+    __syncthreads();
+    if (out) {
+      uint32_t before = holes_first;
+      each_row([&](int i, bool stays) {
+        const bool hole = i < K && !stays;
+        const uint64_t mask = __ballot(hole);
+        if (i < K) out[i] = hole ? sources_of[before + lanes_below(mask)] : i;
+        before += __popcll(mask);
+      });
+      for (int i = K + tid; i < mv.pitch; i += NW * 64) out[i] = -1;
+    }
+    if (!kHeld) __syncthreads();  // the keys have been made for the last time: weights may change
+    if (near) {  // a wave per block that takes rows in
+      const int block_of = lane < (int)moves ? near_holes[lane] >> shift : -1;
+      const int before = lane == 0 ? -2 : near_holes[max(lane - 1, 0)] >> shift;
+      uint64_t firsts = __ballot(lane < (int)moves && block_of != before);
+      for (int x = 0; firsts != 0; x++) {
+        const int first = __ffsll((unsigned long long)firsts) - 1;
+        firsts &= firsts - 1;
+        if (x % NW != wave) continue;
+        const int end = firsts ? __ffsll((unsigned long long)firsts) - 1 : (int)moves;
+        move_block(pl, b, h, near_holes, near_sources, first, end, __builtin_amdgcn_readlane(block_of, first), K, cut, lane);
+      }
+    } else {
+      for (int block = wave; block < kept_blocks; block += NW)
+        if (starts[block] != starts[block + 1])
+          move_block(pl, b, h, holes_of, sources_of, starts[block], starts[block + 1], block, K, cut, lane);
+    }
+  }
 }
 
-// Grid: blocks of the kept rows, heads, K and V.
-template <int NW, int NC>
-__global__ __launch_bounds__(NW * 64) void kv8_move(Kv8Plan pl, const int32_t* __restrict__ n_kept,
-                                                    const int32_t* __restrict__ row_from, int pitch,
-                                                    const float2* __restrict__ cut_scales) {
+// The moves, a wave per block, and row_from_opt.
+constexpr int kMoveWaves = 4, kFewMoves = 64;
+__global__ __launch_bounds__(kMoveWaves * 64) void kv8_move(Kv8Plan pl, const int32_t* __restrict__ n_kept, int32_t* row_from_opt,
+                                                            Moves mv) {
+  __shared__ int32_t row_of[kMoveWaves][128];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int bh = blockIdx.y, b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
-  const int K = n_kept[bh], block = blockIdx.x, rows = 1 << pl.block_shift, first = block << pl.block_shift;
-  const int32_t* from = row_from + (size_t)bh * pitch + first;
-  const int here = min(rows, K - first);  // kept rows of this block
-  bool comes = false, stays = false;
-  for (int r = threadIdx.x; r < here; r += NW * 64) {
-    if (from[r] == first + r) stays = true;
-    else comes = true;
+  const int block = blockIdx.x * kMoveWaves + wave;
+  if (block >= mv.blocks) return;
+  const int32_t* starts = mv.starts + (size_t)bh * (mv.blocks + 1);
+  const int32_t* holes = mv.holes + (size_t)bh * mv.pitch;
+  const int32_t* sources = mv.sources + (size_t)bh * mv.pitch;
+  const int first = starts[block], end = starts[block + 1], K = n_kept[bh];
+  if (first != end) move_block(pl, b, h, holes, sources, first, end, block, K, mv.cut[bh], lane);
+  if (row_from_opt) {
+    const int row0 = block << pl.block_shift, rows = min(1 << pl.block_shift, mv.pitch - row0);
+    for (int r = lane; r < rows; r += 64) row_of[wave][r] = row0 + r < K ? row0 + r : -1;
+    for (int j = first + lane; j < end; j += 64) row_of[wave][holes[j] - row0] = sources[j];
+    int32_t* out = row_from_opt + (size_t)bh * mv.pitch + row0;
+    for (int r = lane; r < rows; r += 64) out[r] = row_of[wave][r];
   }
-  if (!__syncthreads_or(comes)) return;
-  stays = __syncthreads_or(stays);
-  const bool is_v = blockIdx.z != 0;
-  uint8_t* head = (is_v ? pl.v : pl.k) + b * pl.sb + h * pl.sh;
-  float* scale = (is_v ? pl.v_scale : pl.k_scale) + b * pl.ssb + h * pl.ssh;
-  const int cut = K >> pl.block_shift;
-  const float cut_scale = is_v ? cut_scales[bh].y : cut_scales[bh].x;
-  const bool is_cut = block == cut;
-  put_rows<NW, NC>(
-      head + (int64_t)first * pl.st, pl.st, scale + block, is_cut ? cut_scale : scale[block], stays, here, pl.d,
-      [&](int r) { return from[r] == first + r ? kStays : kComes; },
-      [&](int r, int column, float(&x)[16]) {
-        const int f = from[r], fb = f >> pl.block_shift;
-        decode16(*reinterpret_cast<const uint4*>(head + (int64_t)f * pl.st + column), x, fb == cut ? cut_scale : scale[fb]);
-      });
 }
 
 // The shape of a workgroup that holds a block's chunks in registers, four per thread before waves are added: f(waves, chunks).
@@ -319,29 +536,57 @@ hipError_t launch_kv8_append(const Kv8Plan& pl, const void* k_new, const void* v
   return hipGetLastError();
 }
 
-// Workspace: the sources of every head, row_from where the caller has no room for it, the cut blocks' scales.
-size_t kv8_evict_workspace(const Kv8Plan& pl) {
+// Workspace: holes, sources and starts of every head, the cut blocks' scales.
+static Moves moves_in(const Kv8Plan& pl, void* workspace, size_t* bytes) {
   const size_t heads = (size_t)pl.nb * pl.Hkv;
-  return 2 * align256(heads * kv8_most_kept(pl) * sizeof(int32_t)) + align256(heads * sizeof(float2));
+  const int T = 1 << pl.block_shift, pitch = kv8_most_kept(pl), blocks = (pitch + T - 1) / T;
+  char* ws = static_cast<char*>(workspace);
+  size_t at = 0;
+  auto take = [&](size_t n) {
+    char* p = ws ? ws + at : nullptr;
+    at += align256(n);
+    return reinterpret_cast<int32_t*>(p);
+  };
+  Moves mv;
+  mv.pitch = pitch, mv.blocks = blocks;
+  mv.holes = take(heads * pitch * sizeof(int32_t));
+  mv.sources = take(heads * pitch * sizeof(int32_t));
+  mv.starts = take(heads * (blocks + 1) * sizeof(int32_t));
+  mv.cut = reinterpret_cast<float2*>(take(heads * sizeof(float2)));
+  *bytes = at;
+  return mv;
+}
+
+size_t kv8_evict_workspace(const Kv8Plan& pl) {
+  size_t bytes;
+  moves_in(pl, nullptr, &bytes);
+  return bytes;
 }
 
 hipError_t launch_kv8_evict(const Kv8Plan& pl, const int32_t* budgets, int32_t* n_kept, int32_t* row_from, void* workspace,
                             hipStream_t stream) {
-  const int heads = pl.nb * pl.Hkv, pitch = kv8_most_kept(pl), T = 1 << pl.block_shift;
-  char* ws = static_cast<char*>(workspace);
-  int32_t* sources = reinterpret_cast<int32_t*>(ws);
-  ws += align256((size_t)heads * pitch * sizeof(int32_t));
-  if (!row_from) row_from = reinterpret_cast<int32_t*>(ws);
-  ws += align256((size_t)heads * pitch * sizeof(int32_t));
-  float2* cut_scales = reinterpret_cast<float2*>(ws);
-  hipLaunchKernelGGL(kv8_choose, dim3(heads), dim3(1024), 0, stream, pl, budgets, n_kept, row_from, pitch, sources, cut_scales);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  with_block_shape(pl, [&](auto nw, auto nc) {
-    constexpr int NW = decltype(nw)::value, NC = decltype(nc)::value;
-    hipLaunchKernelGGL((kv8_move<NW, NC>), dim3((pitch + T - 1) / T, heads, 2), dim3(NW * 64), 0, stream, pl, n_kept, row_from,
-                       pitch, cut_scales);
-  });
+  size_t bytes;
+  const Moves mv = moves_in(pl, workspace, &bytes);
+  const int heads = pl.nb * pl.Hkv, rows = pl.n_cached + pl.n_block;
+  // A few moves per head (a decoding step's) are made by the workgroup that chose them.
+  const bool fused = rows - mv.pitch <= kFewMoves;
+  auto go = [&](auto vpt, auto nw) {
+    constexpr int VPT = decltype(vpt)::value, NW = decltype(nw)::value;
+    if (fused) hipLaunchKernelGGL((kv8_choose<VPT, NW, true>), dim3(heads), dim3(NW * 64), 0, stream, pl, budgets, n_kept, row_from, mv);
+    else hipLaunchKernelGGL((kv8_choose<VPT, NW, false>), dim3(heads), dim3(NW * 64), 0, stream, pl, budgets, n_kept, row_from, mv);
+  };
+  using std::integral_constant;
+  if (rows <= 1024) go(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  else if (rows <= 4096) go(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+  else if (rows <= 8192) go(integral_constant<int, 8>{}, integral_constant<int, 16>{});
+  else if (rows <= 16384) go(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+  else if (rows <= 24576) go(integral_constant<int, 24>{}, integral_constant<int, 16>{});
+  else if (rows <= 32768) go(integral_constant<int, 32>{}, integral_constant<int, 16>{});
+  else go(integral_constant<int, 0>{}, integral_constant<int, 16>{});
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || fused) return e;
+  hipLaunchKernelGGL(kv8_move, dim3((mv.blocks + kMoveWaves - 1) / kMoveWaves, heads), dim3(kMoveWaves * 64), 0, stream, pl, n_kept,
+                     row_from, mv);
   return hipGetLastError();
 }
 
