@@ -176,7 +176,7 @@ __device__ __forceinline__ void not_numbers(Step<NCH>& s, f32x4 (&acc)[NR][4 * N
 
 // EXACT: d = 64 NCH; a lane's columns of V are then 4 NCH neighbouring ones, else 4 of every 64.
 // Waves per SIMD that the registers are cut for.
-constexpr int token_occupancy(size_t elem, int chunks) { return chunks <= 2 ? (elem == 4 ? 2 : 3) : elem == 4 && chunks > 3 ? 1 : 2; }
+constexpr int token_occupancy(size_t elem, int chunks) { return chunks <= 1 ? 3 : chunks <= (elem == 4 ? 2 : 3) ? 2 : 1; }
 
 template <typename T, int NCH, bool EXACT, int NR>
 __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * NR)) void kv8_attention_tokens(Kv8Plan pl, const T* __restrict__ q, T* __restrict__ out,
@@ -229,14 +229,16 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
     for (int j = 0; j < NT; j++) acc[r][j] = f32x4{0, 0, 0, 0};
   }
 
-  auto load = [&](Step<NCH>& s, int tile) {
+  // INSIDE: all keys of the tile are there, and seen by every row
+  auto load = [&](auto inside, Step<NCH>& s, int tile) {
+    constexpr bool INSIDE = decltype(inside)::value;
     const int key0 = tile * kTokenKeys;
 #pragma unroll
     for (int a = 0; a < 2; a++) {
-      const int block = min(key0 + 16 * a, n - 1) >> pl.block_shift;
+      const int block = (INSIDE ? key0 + 16 * a : min(key0 + 16 * a, n - 1)) >> pl.block_shift;
       s.ks[a] = ks[block], s.vs[a] = vs[block];
     }
-    if (key0 + kTokenKeys <= n) {
+    if constexpr (INSIDE) {
       const uint8_t* kt = kbase + (int64_t)key0 * pitch;
       const uint8_t* vt = vbase + (int64_t)key0 * pitch;
 #pragma unroll
@@ -269,9 +271,9 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
     }
   };
 
-  auto work = [&](Step<NCH>& s, int tile) {
+  auto work = [&](auto inside, Step<NCH>& s, int tile) {
+    constexpr bool INSIDE = decltype(inside)::value;
     const int key0 = tile * kTokenKeys;
-    const bool masked = key0 + kTokenKeys > all_see;
     // logits, in base 2: lane (query m16, g) has the keys 16 a + 4 g + i
     float x[NR][8];
 #pragma unroll
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
 #pragma unroll
         for (int i = 0; i < 4; i++) x[r][4 * a + i] = z[r][i] * by;
     }
-    if (masked) {
+    if constexpr (!INSIDE) {
 #pragma unroll
       for (int r = 0; r < NR; r++)
 #pragma unroll
@@ -341,7 +343,8 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
         for (int part = 0; part < PP; part++) pf[r][part][i] = p[part];
       }
     }
-    if (masked && pl.causal && pl.p > 1) not_numbers<NCH, NR>(s, acc, key0, g, last);
+    if constexpr (!INSIDE)
+      if (pl.causal && pl.p > 1) not_numbers<NCH, NR>(s, acc, key0, g, last);
     // out^T += V^T P^T.  Bytes of one column in four keys: two byte permutations make pairs of keys of two columns each.
 #pragma unroll
     for (int c = 0; c < NCH; c++)
@@ -368,13 +371,26 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
   };
 
   {
-    Step<NCH> now, next;
+    // two steps' rows on their way: one is asked for as soon as its registers are free
+    Step<NCH> one, two;
+    const std::true_type in;
+    const int inside_end = min(end, all_see / kTokenKeys);
     int tile = split * per_split + wave;
-    if (tile < end) load(now, tile);
-    for (; tile < end; tile += kTokenWaves) {
-      if (tile + kTokenWaves < end) load(next, tile + kTokenWaves);
-      work(now, tile);
-      now = next;
+    if (tile < inside_end) load(in, one, tile);
+    if (tile + kTokenWaves < inside_end) load(in, two, tile + kTokenWaves);
+    for (; tile < inside_end; tile += 2 * kTokenWaves) {
+      work(in, one, tile);
+      if (tile + 2 * kTokenWaves < inside_end) load(in, one, tile + 2 * kTokenWaves);
+      if (tile + kTokenWaves >= inside_end) {
+        tile += kTokenWaves;
+        break;
+      }
+      work(in, two, tile + kTokenWaves);
+      if (tile + 3 * kTokenWaves < inside_end) load(in, two, tile + 3 * kTokenWaves);
+    }
+    for (; tile < end; tile += kTokenWaves) {  // the last ones
+      load(std::false_type{}, one, tile);
+      work(std::false_type{}, one, tile);
     }
   }
 
