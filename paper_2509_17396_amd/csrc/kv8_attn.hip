@@ -245,12 +245,19 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
       for (int a = 0; a < 2; a++)
 #pragma unroll
         for (int c = 0; c < NCH; c++)
-          s.k[a][c] = *reinterpret_cast<const uint4*>(kt + (16 * a + m16) * pitch + chunk_of(c) * 16);
+          s.k[a][c] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(kt + (16 * a + m16) * pitch + chunk_of(c) * 16)));
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const uint8_t* row = vt + ((i >> 2) * 16 + 4 * g + (i & 3)) * pitch;
+        if constexpr (EXACT && NCH != 3) {
+          typedef __attribute__((ext_vector_type(NCH))) uint32_t columns;
+          const columns u = __builtin_nontemporal_load(reinterpret_cast<const columns*>(row + column_of(0)));
 #pragma unroll
-        for (int c = 0; c < NCH; c++) s.v[i][c] = *reinterpret_cast<const uint32_t*>(row + column_of(c));
+          for (int c = 0; c < NCH; c++) s.v[i][c] = u[c];
+        } else {
+#pragma unroll
+          for (int c = 0; c < NCH; c++) s.v[i][c] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(row + column_of(c)));
+        }
       }
     } else {  // rows behind the last one: K of the last one again, V 0
 #pragma unroll
@@ -1020,8 +1027,10 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 TokenRoom token_room(const Kv8Plan& pl, void* workspace, size_t* bytes) {
   const int64_t heads = (int64_t)pl.nb * pl.Hkv;
   const int tiles = (pl.n_cached + pl.n_block + kTokenKeys - 1) / kTokenKeys;
-  // four workgroups for every CU, each with two steps a wave at least
-  int64_t splits = (4 * kComputeUnits + heads - 1) / heads;
+  // a round of resident workgroups, each with two steps a wave at least
+  const int64_t slots = kComputeUnits * token_occupancy(pl.dtype == EPICACHE_DTYPE_F32 ? 4 : 2, (pl.d + 63) / 64 * ((pl.R + 15) / 16));
+  int64_t splits = slots / heads;
+  if (splits > 0 && tiles / splits >= 16 * kTokenWaves) splits *= 2;
   splits = std::max<int64_t>(1, std::min<int64_t>({splits, tiles / (2 * kTokenWaves), kMostSplits}));
   TokenRoom room = {(int)splits, tiles * kTokenKeys, nullptr, nullptr, nullptr};
   char* ws = static_cast<char*>(workspace);
