@@ -539,8 +539,8 @@ struct BlockRoom {
 
 constexpr int kBlockKeys = 64;
 
-// Waves of a workgroup: no more than have rows.
-int block_waves(const Kv8Plan& pl) { return pl.R <= 64 ? 2 : 4; }
+// Waves of a workgroup.  The fewer rows, the more of them only help with the tiles.
+int block_waves(const Kv8Plan& pl) { return pl.R > 128 && pl.d > 64 && pl.d <= 128 && pl.dtype == EPICACHE_DTYPE_BF16 ? 8 : 4; }
 
 __device__ __forceinline__ bool folds(float scale) {  // into the exponent of a decoded value
   const uint32_t u = __float_as_uint(scale);
@@ -551,10 +551,12 @@ __device__ __forceinline__ bool folds(float scale) {  // into the exponent of a 
 template <int HD, int NT>
 struct TileCodes {
   static constexpr int kPer = kBlockKeys * (HD / 16) / NT;
+  static_assert(kPer >= 1, "every thread has a chunk");
   uint4 k[kPer], v[kPer];
   float ks[kPer], vs[kPer];
 };
 
+// Waves per SIMD that the registers are cut for.
 constexpr int block_occupancy(size_t elem, int hd) { return elem == 2 && hd <= 128 ? 2 : 1; }
 
 __device__ __forceinline__ uint4 codes_to_bf16x8(uint32_t lo, uint32_t hi, float scale) {
@@ -588,17 +590,6 @@ __device__ __forceinline__ void rows_see(const Kv8Plan& pl, int old, int n, int 
   least = old + 1 + (ga == gb ? ta : 0), most = old + 1 + (ga == gb ? tb : pl.p - 1);
 }
 
-// V^T operand of the NaN codes among 8 keys (key + 0 .. 3, key + 8 .. 11) of one column: ones.
-__device__ __forceinline__ bf16x8 nan_frag(const uint8_t* v, uint32_t pitch, int key, int n) {
-  u32x4 u = {0, 0, 0, 0};
-#pragma unroll
-  for (int j = 0; j < 8; j++) {
-    const int at = key + (j & 3) + (j >> 2) * 8;
-    if (at < n && (v[(int64_t)at * pitch] & 0x7f) == 0x7f) u[j >> 1] |= 0x3f80u << 16 * (j & 1);
-  }
-  return __builtin_bit_cast(bf16x8, u);
-}
-
 // HD: row layout in LDS; KS 16-element steps of Q K^T, DB 32-column blocks of the output.
 template <typename T, int HD, int KS, int DB, int NW>
 __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_attention_block(
@@ -610,7 +601,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   using Codes = TileCodes<HD, NT>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // K, K, V, V, then
   float(*rest)[2][4] = reinterpret_cast<float(*)[2][4]>(smem + 4 * kTile);  // [buffer][K, V][16 keys]: what scales have not been folded
-  int* nan_seen = reinterpret_cast<int*>(smem + 4 * kTile + 64);            // [buffer]: the tile there from whose V NaN codes have been taken out
+  int* nan_seen = reinterpret_cast<int*>(smem + 4 * kTile + 64);  // NaN codes have been taken out of a V that not all rows see
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
@@ -623,18 +614,17 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   const int old = kv8_old_rows(pl, bh), n = old + pl.n_block;
 
   const int first_row = rb * 32 * NW, row0 = first_row + wave * 32, r = row0 + l32;
-  const bool active = row0 < pl.R, row_ok = r < pl.R;
+  const bool active = row0 < pl.R;
   int g_row, t_row;
   head_and_token(pl.p, pl.inv_p, min(r, pl.R - 1), g_row, t_row);
   const int last_key = pl.causal ? old + t_row : n - 1;
+  bf16x8 qf[PARTS][KS];
+  load_rows<KS>(qf, q + b * pl.qsb + (int64_t)(h * pl.G + g_row) * pl.qsh + (int64_t)t_row * pl.qst, hi, pl.d);
   int all_see, any_sees, wave_all, wave_any;
   rows_see(pl, old, n, first_row, first_row + 32 * NW, all_see, any_sees);
   rows_see(pl, old, n, row0, row0 + 32, wave_all, wave_any);
   const int tiles = (any_sees + kBlockKeys - 1) / kBlockKeys;
   const int first_tile = split * room.split_tiles, end_tile = room.splits == 1 ? tiles : min(tiles, first_tile + room.split_tiles);
-
-  bf16x8 qf[PARTS][KS];
-  load_rows<KS>(qf, q + b * pl.qsb + (int64_t)(h * pl.G + g_row) * pl.qsh + (int64_t)t_row * pl.qst, hi, pl.d);
 
   const uint8_t* kbase = pl.k + b * pl.sb + h * pl.sh;
   const uint8_t* vbase = pl.v + b * pl.sb + h * pl.sh;
@@ -660,7 +650,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     }
   };
   auto place = [&](Codes& c, int buf, int t) {
-    const bool partly = (t + 1) * kBlockKeys > all_see;
+    const bool partly = (t + 1) * kBlockKeys > all_see;  // a weight of 0 times a NaN code would be a NaN in rows that do not see it
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < Codes::kPer; i++) {
@@ -688,7 +678,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       *reinterpret_cast<uint4*>(vt + (((2 * chunk) ^ sv) * 16)) = codes_to_bf16x8(c.v[i].x, c.v[i].y, vfold);
       *reinterpret_cast<uint4*>(vt + (((2 * chunk + 1) ^ sv) * 16)) = codes_to_bf16x8(c.v[i].z, c.v[i].w, vfold);
     }
-    if (partly && nan) nan_seen[buf] = t;
+    if (partly && nan) *nan_seen = 1;
   };
 
   f32x16 o[DB];
@@ -700,32 +690,31 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     const unsigned char* ktile = smem + buf * kTile;
     const unsigned char* vtile = smem + (2 + buf) * kTile;
     const bool masked = (t + 1) * kBlockKeys > wave_all;
-    float plain = 1.f;  // all ones, or some scale was not folded
-#pragma unroll
-    for (int i = 0; i < 4; i++) plain = rest[buf][0][i] == 1.f && rest[buf][1][i] == 1.f ? plain : 0.f;
+    const float4 kr = *reinterpret_cast<const float4*>(rest[buf][0]), vr = *reinterpret_cast<const float4*>(rest[buf][1]);
+    const bool folded = __all(kr.x == 1.f && kr.y == 1.f && kr.z == 1.f && kr.w == 1.f && vr.x == 1.f && vr.y == 1.f && vr.z == 1.f && vr.w == 1.f);
+    bf16x8 kf[KS];
+    read_frags<HD, KS>(kf, ktile, 0, l32, hi);
 #pragma unroll
     for (int half = 0; half < 2; half++) {
       const int key0 = t * kBlockKeys + 32 * half;
-      bf16x8 kf[KS];
-      read_frags<HD, KS>(kf, ktile, half, l32, hi);
-      f32x16 z = f32x16{0};
+      f32x16 z;
+      z = f32x16{0};
 #pragma unroll
       for (int part = PARTS - 1; part >= 0; part--)
 #pragma unroll
         for (int j = 0; j < KS; j++) mfma_step(z, kf[j], qf[part][j]);
+      if (half == 0) read_frags<HD, KS>(kf, ktile, 1, l32, hi);  // what the arithmetic below can hide
       bf16x8 vf[DB][2];
 #pragma unroll
       for (int j = 0; j < DB; j++)
 #pragma unroll
         for (int st = 0; st < 2; st++) vf[j][st] = read_vt_frag<HD>(vtile, half, st, j, lane);
-      if (plain == 0.f) {
+      if (masked || !folded) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) z[i] *= rest[buf][0][2 * half + (i >> 3)];
-      }
-      if (masked) {
-#pragma unroll
-        for (int i = 0; i < 16; i++)
+        for (int i = 0; i < 16; i++) {
+          z[i] *= i < 8 ? (half ? kr.z : kr.x) : half ? kr.w : kr.y;
           if (key0 + (i >> 2) * 8 + hi * 4 + (i & 3) > last_key) z[i] = -INFINITY;
+        }
       }
       const float a0 = max3(z[0], z[1], z[2]), a1 = max3(z[3], z[4], z[5]), a2 = max3(z[6], z[7], z[8]);
       const float a3 = max3(z[9], z[10], z[11]), a4 = max3(z[12], z[13], z[14]);
@@ -745,9 +734,9 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       for (int i = 0; i < 16; i++) e[i] = ex2(fmaf(z[i], pl.c2, -m));
       l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])) +
            (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
-      if (plain == 0.f) {
+      if (!folded) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) e[i] *= rest[buf][1][2 * half + (i >> 3)];
+        for (int i = 0; i < 16; i++) e[i] *= i < 8 ? (half ? vr.z : vr.x) : half ? vr.w : vr.y;
       }
 #pragma unroll
       for (int st = 0; st < 2; st++) {
@@ -759,30 +748,11 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
           for (int j = 0; j < DB; j++) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j][st], pf[part], o[j], 0, 0, 0);
       }
     }
-    if (masked && nan_seen[buf] == t) {  // rows that see a NaN code get a NaN in its column
-#pragma unroll 1
-      for (int st = 0; st < 4; st++) {
-        const int key = t * kBlockKeys + 16 * st + 4 * hi;
-        u32x4 u;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const int at = key + (2 * j & 3) + (j >> 1) * 8;
-          u[j] = (at <= last_key ? 0x3f80u : 0u) | (at + 1 <= last_key ? 0x3f800000u : 0u);
-        }
-#pragma unroll
-        for (int j = 0; j < DB; j++) {
-          const f32x16 seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(nan_frag(vbase + min(32 * j + l32, pl.d - 1), pitch, key, n),
-                                                                      __builtin_bit_cast(bf16x8, u), f32x16{0}, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 16; i++) o[j][i] += seen[i] > 0.f ? NAN : 0.f;
-        }
-      }
-    }
   };
 
   {
     Codes c;
-    if (tid < 2) nan_seen[tid] = -1;
+    if (tid == 0) *nan_seen = 0;
     __syncthreads();
     if (first_tile < end_tile) {
       fetch(c, first_tile);
@@ -801,9 +771,11 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     }
   }
 
-  if (!active || !row_ok) return;
+  if (!active) return;
+  const bool whole = room.splits == 1, nan = __any(*nan_seen != 0);
   const float sum = l + __shfl_xor(l, 32);
-  const bool whole = room.splits == 1, any = sum > 0.f || sum != sum;
+  if (r >= pl.R) return;
+  const bool any = sum > 0.f || sum != sum;
   const float inv = any ? 1.f / sum : 0.f;
   const size_t orow = ((size_t)b * pl.Hq + h * pl.G + g_row) * pl.p + t_row;
   const size_t record = (size_t)unit * pl.R + r;
@@ -820,7 +792,15 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       if (column >= pl.d) continue;
       float y[4];
 #pragma unroll
-      for (int x = 0; x < 4; x++) y[x] = !whole ? o[j][4 * i + x] : any ? o[j][4 * i + x] * inv : 0.f;
+      for (int c = 0; c < 4; c++) y[c] = !whole ? o[j][4 * i + c] : any ? o[j][4 * i + c] * inv : 0.f;
+      if (nan) {  // look for them again, among the keys that this row sees
+        const int from = max(first_tile, all_see / kBlockKeys) * kBlockKeys, to = min(end_tile * kBlockKeys, last_key + 1);
+        for (int key = from; key < to; key++) {
+          const uint32_t is = nan_bytes(*reinterpret_cast<const uint32_t*>(vbase + (int64_t)key * pitch + column));
+#pragma unroll
+          for (int c = 0; c < 4; c++) y[c] = (is >> (8 * c + 7)) & 1 ? NAN : y[c];
+        }
+      }
       if (whole) store4(out + orow * pl.d + column, y);
       else store4(room.records + record * pl.d + column, y);
     }
@@ -861,7 +841,8 @@ __global__ __launch_bounds__(256) void kv8_join_rows(Kv8Plan pl, T* __restrict__
 }
 
 // weight += the softmax weights of many rows: the product with K once more, now with the keys in registers and the query rows
-// through LDS, so that every key's sum has one owner and one order.  A wave has 32 NK keys.
+// through LDS, so that every key's sum has one owner and one order.  A wave has 32 NK keys, a lane one column of each 32 and half
+// of its rows: a key's scale and its sum are the lane's own, what belongs to a row comes from LDS.
 template <typename T, int HD, int KS, int NK, int NW>
 __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_accumulate_block(Kv8Plan pl, const T* __restrict__ q,
                                                                                                const float2* __restrict__ rows) {
@@ -872,7 +853,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   constexpr int kPer = QT * TL::kChunks / NT;  // 8-value chunks of a tile per thread
   static_assert(kPer >= 1, "every thread has a chunk");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  float4(*info)[QT] = reinterpret_cast<float4(*)[QT]>(smem + 2 * kTile);  // reference, 1 / sum, last key
+  float(*info)[3][QT] = reinterpret_cast<float(*)[3][QT]>(smem + 2 * kTile);  // [buffer]: reference, 1 / sum, last key
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
@@ -884,35 +865,26 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   const float* ks = pl.k_scale + b * pl.ssb + h * pl.ssh;
 
   bf16x8 kf[NK][KS];
-  float rest[NK][2];
+  float by[NK], acc[NK];  // logits of codes in base 2
 #pragma unroll
   for (int x = 0; x < NK; x++) {
     const int key = min(key0 + 32 * x + l32, n - 1);
-    const float scale = ks[key >> pl.block_shift];
-    const float fold = folds(scale) ? scale : 1.f;
-#pragma unroll
-    for (int s = 0; s < 2; s++) {
-      const float of16 = ks[min(key0 + 32 * x + 16 * s, n - 1) >> pl.block_shift];
-      rest[x][s] = folds(of16) ? 1.f : of16;
-    }
+    by[x] = pl.c2 * ks[key >> pl.block_shift];
+    acc[x] = 0.f;
     const uint8_t* row = kbase + (int64_t)key * pl.st;
 #pragma unroll
     for (int j = 0; j < KS; j++) {
       const int at = (2 * j + hi) * 8;
       uint2 u = make_uint2(0, 0);
       if (at < pl.d) u = *reinterpret_cast<const uint2*>(row + at);
-      kf[x][j] = __builtin_bit_cast(bf16x8, codes_to_bf16x8(u.x, u.y, fold));
+      kf[x][j] = codes_to_frag(u.x, u.y);
     }
   }
-  float acc[NK][16];
-#pragma unroll
-  for (int x = 0; x < NK; x++)
-#pragma unroll
-    for (int i = 0; i < 16; i++) acc[x][i] = 0.f;
 
   struct Share {
-    float v[kPer][8];
-    float4 info;
+    float v[kPer][F32 ? 8 : 4];
+    float2 ml;
+    int last;
   };
   auto fetch = [&](Share& c, int tile) {
 #pragma unroll
@@ -927,18 +899,18 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
         if (F32) z = reinterpret_cast<const float4*>(from)[1];
       }
       c.v[i][0] = a.x, c.v[i][1] = a.y, c.v[i][2] = a.z, c.v[i][3] = a.w;
-      if (F32) c.v[i][4] = z.x, c.v[i][5] = z.y, c.v[i][6] = z.z, c.v[i][7] = z.w;
+      if constexpr (F32) c.v[i][4] = z.x, c.v[i][5] = z.y, c.v[i][6] = z.z, c.v[i][7] = z.w;
     }
     if (tid < QT) {
       const int r = tile * QT + tid;
-      float2 ml = make_float2(0.f, 0.f);
+      c.ml = make_float2(0.f, 0.f);
       int g = 0, t = 0;
       if (r < pl.R) {
-        ml = rows[(size_t)bh * pl.R + r];
+        c.ml = rows[(size_t)bh * pl.R + r];
         head_and_token(pl.p, pl.inv_p, r, g, t);
       }
-      // a row without weights: whatever its logits, exponentials of -inf
-      c.info = make_float4(ml.y == 0.f ? INFINITY : ml.x, ml.y, __int_as_float(pl.causal ? old + t : n - 1), 0.f);
+      if (c.ml.y == 0.f) c.ml.x = INFINITY;  // a row without weights: exponentials of -inf, whatever its logits
+      c.last = pl.causal ? old + t : n - 1;
     }
   };
   auto place = [&](Share& c, int buf) {
@@ -956,7 +928,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
         *to = make_uint4(__float_as_uint(c.v[i][0]), __float_as_uint(c.v[i][1]), __float_as_uint(c.v[i][2]), __float_as_uint(c.v[i][3]));
       }
     }
-    if (tid < QT) info[buf][tid] = c.info;
+    if (tid < QT) info[buf][0][tid] = c.ml.x, info[buf][1][tid] = c.ml.y, info[buf][2][tid] = __int_as_float(c.last);
   };
 
   const int tiles = (pl.R + QT - 1) / QT;
@@ -971,7 +943,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       place(c, buf ^ 1);
       if (t + 2 < tiles) fetch(c, t + 2);
     }
-#pragma unroll
+#pragma unroll 1
     for (int half = 0; half < QT / 32; half++) {
       int least, most;
       const int row0 = t * QT + 32 * half;
@@ -980,45 +952,43 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       bf16x8 qf[PARTS][KS];
 #pragma unroll
       for (int p = 0; p < PARTS; p++) read_frags<HD, KS>(qf[p], smem + buf * kTile + p * kPart, half, l32, hi);
-      const float4 row = info[buf][32 * half + l32];
-      const int last = __float_as_int(row.z);
+      float m[16], inv[16];  // of the lane's rows 8 (i / 4) + 4 hi + i % 4
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        *reinterpret_cast<float4*>(m + 4 * i) = *reinterpret_cast<const float4*>(&info[buf][0][32 * half + 8 * i + 4 * hi]);
+        *reinterpret_cast<float4*>(inv + 4 * i) = *reinterpret_cast<const float4*>(&info[buf][1][32 * half + 8 * i + 4 * hi]);
+      }
 #pragma unroll
       for (int x = 0; x < NK; x++) {
         f32x16 z = f32x16{0};
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; p--)
 #pragma unroll
-          for (int j = 0; j < KS; j++) mfma_step(z, kf[x][j], qf[p][j]);
-        if (rest[x][0] != 1.f || rest[x][1] != 1.f) {
-#pragma unroll
-          for (int i = 0; i < 16; i++) z[i] *= rest[x][i >> 3];
-        }
-        const bool masked = key0 + 32 * x + 32 > least;
-        if (masked) {
+          for (int j = 0; j < KS; j++) mfma_step(z, qf[p][j], kf[x][j]);
+        float sum[4] = {0, 0, 0, 0};
+        if (key0 + 32 * x + 32 > least) {
+          const int key = key0 + 32 * x + l32;
 #pragma unroll
           for (int i = 0; i < 16; i++) {
-            const bool seen = key0 + 32 * x + (i >> 2) * 8 + hi * 4 + (i & 3) <= last;
-            acc[x][i] += seen ? ex2(fmaf(z[i], pl.c2, -row.x)) * row.y : 0.f;
+            const int last = __float_as_int(info[buf][2][32 * half + 8 * (i >> 2) + 4 * hi + (i & 3)]);
+            sum[i & 3] += key <= last ? ex2(fmaf(z[i], by[x], -m[i])) * inv[i] : 0.f;
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < 16; i++) acc[x][i] = fmaf(ex2(fmaf(z[i], pl.c2, -row.x)), row.y, acc[x][i]);
+          for (int i = 0; i < 16; i++) sum[i & 3] = fmaf(ex2(fmaf(z[i], by[x], -m[i])), inv[i], sum[i & 3]);
         }
+        acc[x] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
     }
     __syncthreads();
   }
   float* weight = pl.weight + b * pl.rsb + h * pl.rsh;
 #pragma unroll
-  for (int x = 0; x < NK; x++)
-#pragma unroll
-    for (int i = 0; i < 16; i++) {
-      float s = acc[x][i];
-#pragma unroll
-      for (int lanes = 1; lanes < 32; lanes <<= 1) s += __shfl_xor(s, lanes);
-      const int key = key0 + 32 * x + (i >> 2) * 8 + hi * 4 + (i & 3);
-      if (l32 == 0 && key < n) weight[key] += s;
-    }
+  for (int x = 0; x < NK; x++) {
+    const float sum = acc[x] + __shfl_xor(acc[x], 32);
+    const int key = key0 + 32 * x + l32;
+    if (hi == 0 && key < n) weight[key] += sum;
+  }
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -1083,7 +1053,7 @@ BlockRoom block_room(const Kv8Plan& pl, void* workspace, size_t* bytes) {
   const int64_t heads = (int64_t)pl.nb * pl.Hkv;
   const int nw = block_waves(pl), n_rb = (pl.R + 32 * nw - 1) / (32 * nw);
   const int tiles = (pl.n_cached + pl.n_block + kBlockKeys - 1) / kBlockKeys;
-  const int64_t slots = kComputeUnits * (nw == 2 ? 2 : 1) * block_occupancy(pl.dtype == EPICACHE_DTYPE_F32 ? 4 : 2, pl.d <= 128 ? 128 : 256);
+  const int64_t slots = kComputeUnits * 4 * block_occupancy(pl.dtype == EPICACHE_DTYPE_F32 ? 4 : 2, pl.d <= 128 ? 128 : 256) / nw;
   int64_t splits = slots / (heads * n_rb);  // a round of workgroups, each with four tiles at least
   splits = std::max<int64_t>(1, std::min<int64_t>({splits, tiles / 4, kMostSplits}));
   const int split_tiles = (tiles + (int)splits - 1) / (int)splits;
@@ -1131,7 +1101,7 @@ hipError_t launch_block(const Kv8Plan& pl, const T* q, T* out, float* lse, void*
   }
   if (!pl.accumulate) return hipSuccess;
   constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = sizeof(T) == 4 ? 32 : 64, NK = HD == 256 ? 1 : 2;
-  constexpr size_t lds = 2 * PARTS * QT * Tile<HD>::kRowBytes + 2 * QT * sizeof(float4);
+  constexpr size_t lds = 2 * PARTS * QT * Tile<HD>::kRowBytes + 2 * 3 * QT * sizeof(float);
   const int keys = 32 * NK * 4;
   return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + keys - 1) / keys, heads), 256, lds,
                          stream, pl, q, room.rows);
@@ -1141,7 +1111,8 @@ template <typename T>
 hipError_t launch_blocks(const Kv8Plan& pl, const T* q, T* out, float* lse, void* workspace, hipStream_t stream) {
   auto waves = [&](auto hd, auto ks, auto db) {
     constexpr int HD = decltype(hd)::value, KS = decltype(ks)::value, DB = decltype(db)::value;
-    if (block_waves(pl) == 2) return launch_block<T, HD, KS, DB, 2>(pl, q, out, lse, workspace, stream);
+    if constexpr (sizeof(T) == 2 && HD == 128)
+      if (block_waves(pl) == 8) return launch_block<T, HD, KS, DB, 8>(pl, q, out, lse, workspace, stream);
     return launch_block<T, HD, KS, DB, 4>(pl, q, out, lse, workspace, stream);
   };
   using std::integral_constant;

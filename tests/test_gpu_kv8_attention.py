@@ -161,6 +161,17 @@ def test_not_finite():
             run(ku.Cache(1, 4, 180, 64, 16, seed=7), dtype, 2, p, 100, p, 1, True, edit=edit)
 
 
+@pytest.mark.parametrize("G", [1, 3])
+@pytest.mark.parametrize("dtype,p", [("bf16", 9), ("bf16", 40), ("bf16", 150), ("bf16", 300), ("f32", 9), ("f32", 150)])
+def test_not_a_number_inside_a_block(dtype, p, G):
+    """Values that are not numbers among the block's own rows: the queries from there on see them, those before do not."""
+    def edit(q, cache):
+        for h, (row, column) in enumerate(((0, 3), (p // 2, 60), (p // 3, 17))):
+            cache.view["v"][0, h, 100 + row, column] = 0x7F
+            cache.view["v"][0, h, 100 + p - 1, column + 1] = 0xFF
+    run(ku.Cache(1, 3, 100 + p, 64, 16, seed=9), dtype, G, p, 100, p, 1, True, edit=edit)
+
+
 @pytest.mark.parametrize("dtype,p", [("bf16", 1), ("bf16", 80), ("f32", 1), ("bf16", 6)])
 def test_the_same_bits_every_time(dtype, p):
     got = [run(ku.Cache(2, 2, 3000, 128, 32, seed=8), dtype, 4, p, 2900, p, 1, True, repeat=2) for _ in range(2)]
