@@ -527,8 +527,8 @@ __global__ __launch_bounds__(256) void kv8_join_tokens(Kv8Plan pl, T* __restrict
 // ---- Many query rows per KV head (patches, prefilled blocks): tiles of keys through LDS, shared by the waves of a workgroup.
 //
 // A wave owns 32 query rows.  Tiles of 64 rows of K and V come from memory as codes, one tile ahead, are decoded to bf16 (exactly,
-// with their scale where it is a power of two) by whoever fetched them and lie in LDS double buffered, K as the scoring kernels have it and
-// V as the patch attention's transposing loads want it.  Per 32 keys: S^T = K Q^T, an online softmax, O^T += V^T P^T.
+// with their scale where it is a power of two) by whoever fetched them and lie in LDS double
+// buffered.  Per 32 keys: S^T = K Q^T, an online softmax, O^T += V^T P^T.
 
 struct BlockRoom {
   int splits, split_tiles;  // workgroups that share the keys of a row, and the tiles of each
@@ -547,13 +547,47 @@ __device__ __forceinline__ bool folds(float scale) {  // into the exponent of a 
   return (u & 0x7fffffu) == 0 && u != 0;
 }
 
+// Rows in LDS are padded, not swizzled, so that every operand is at one lane address plus an immediate: by 16 bytes where a
+// fragment's 16 lanes read 16 rows, by 32 where the transposing load's read 32 bytes of 4 rows.  Both without bank conflicts.
+template <int HD>
+constexpr int row_pitch() { return HD * 2 + 16; }
+template <int HD>
+constexpr int value_pitch() { return HD * 2 + 32; }
+
+// Operand fragments of 32 rows; `lane_base`: row l % 32, byte 16 (l / 32).
+template <int HD, int KS>
+__device__ __forceinline__ void read_rows(bf16x8 (&f)[KS], const unsigned char* lane_base, int sub) {
+#pragma unroll
+  for (int j = 0; j < KS; j++) f[j] = as_frag(*reinterpret_cast<const uint4*>(lane_base + sub * 32 * row_pitch<HD>() + j * 32));
+}
+// A operand of O^T += V^T P^T as read_vt_frag has it; `lane_base`: see value_base.
+__device__ __forceinline__ int value_base(int pitch, int lane) {
+  const int s = lane & 15, gh = (lane >> 4) & 1, hi = lane >> 5;
+  return (4 * hi + (s >> 2)) * pitch + gh * 32 + (s & 3) * 8;
+}
+template <int HD>
+__device__ __forceinline__ bf16x8 read_values(const unsigned char* lane_base, int half, int step, int block) {
+  s16x4 part[2];
+#pragma unroll
+  for (int g = 0; g < 2; g++) {
+    const unsigned char* p = lane_base + (32 * half + 16 * step + 8 * g) * value_pitch<HD>() + block * 64;
+    part[g] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)LDS_PTR(p));
+  }
+  typedef __attribute__((ext_vector_type(8))) short s16x8;
+  const s16x8 both = {part[0][0], part[0][1], part[0][2], part[0][3], part[1][0], part[1][1], part[1][2], part[1][3]};
+  return __builtin_bit_cast(bf16x8, both);
+}
+// Bytes of the two buffers of K and V tiles.
+template <int HD>
+constexpr int block_tiles_bytes() { return 2 * kBlockKeys * (row_pitch<HD>() + value_pitch<HD>()); }
+
 // Thread's share of a tile on its way to LDS: 16-code chunks tid, tid + NT, .. of the tile's rows, K and V.
 template <int HD, int NT>
 struct TileCodes {
   static constexpr int kPer = kBlockKeys * (HD / 16) / NT;
   static_assert(kPer >= 1, "every thread has a chunk");
   uint4 k[kPer], v[kPer];
-  float ks[kPer], vs[kPer];
+  float ks[kPer], vs[kPer];  // of the 16 keys that a wave's chunks lie in: wave-uniform
 };
 
 // Waves per SIMD that the registers are cut for.
@@ -594,14 +628,15 @@ __device__ __forceinline__ void rows_see(const Kv8Plan& pl, int old, int n, int 
 template <typename T, int HD, int KS, int DB, int NW>
 __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_attention_block(
     Kv8Plan pl, const T* __restrict__ q, T* __restrict__ out, float* __restrict__ lse, BlockRoom room) {
-  using TL = Tile<HD>;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int PARTS = F32 ? 3 : 1, NT = NW * 64;
-  constexpr int kTile = kBlockKeys * TL::kRowBytes;
+  constexpr int kKTile = kBlockKeys * row_pitch<HD>(), kVTile = kBlockKeys * value_pitch<HD>();
   using Codes = TileCodes<HD, NT>;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];  // K, K, V, V, then
-  float(*rest)[2][4] = reinterpret_cast<float(*)[2][4]>(smem + 4 * kTile);  // [buffer][K, V][16 keys]: what scales have not been folded
-  int* nan_seen = reinterpret_cast<int*>(smem + 4 * kTile + 64);  // NaN codes have been taken out of a V that not all rows see
+  unsigned char* const more = smem + block_tiles_bytes<HD>();
+  float(*rest)[2][4] = reinterpret_cast<float(*)[2][4]>(more);  // [buffer][K, V][16 keys]: what scales have not been folded
+  int* unfolded = reinterpret_cast<int*>(more + 64);            // [buffer]: the last tile there with such a scale
+  int* nan_seen = reinterpret_cast<int*>(more + 72);            // NaN codes have been taken out of a V that not all rows see
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
@@ -633,32 +668,45 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   const uint32_t pitch = (uint32_t)pl.st;
 
   // a row of the tile has HD / 16 chunks, of which the first d / 16 are there
+  const int my_row = tid / (HD / 16), my_chunk = tid % (HD / 16);
+  constexpr int kRowsApart = NT / (HD / 16);  // from a thread's chunk to its next
+  const bool in_row = my_chunk * 16 < pl.d;
+  const uint32_t my_offset = (uint32_t)my_row * pitch + (in_row ? my_chunk * 16 : 0);
   auto fetch = [&](Codes& c, int t) {
     const int key0 = t * kBlockKeys;
+    const uint8_t* kt = kbase + (int64_t)key0 * pitch;
+    const uint8_t* vt = vbase + (int64_t)key0 * pitch;
 #pragma unroll
     for (int i = 0; i < Codes::kPer; i++) {
-      const int at = tid + i * NT, row = at / (HD / 16), chunk = at % (HD / 16);
-      const int key = key0 + row;
-      c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
-      const int block = min(key, n - 1) >> pl.block_shift;
+      const int row = my_row + i * kRowsApart;
+      const int block = min(key0 + (__builtin_amdgcn_readfirstlane(row) & ~15), n - 1) >> pl.block_shift;
       c.ks[i] = ks[block], c.vs[i] = vs[block];
-      if (key < n && chunk * 16 < pl.d) {
-        const int64_t from = (int64_t)key * pitch + chunk * 16;
-        c.k[i] = *reinterpret_cast<const uint4*>(kbase + from);
-        c.v[i] = *reinterpret_cast<const uint4*>(vbase + from);
+      if (key0 + kBlockKeys <= n) {
+        c.k[i] = *reinterpret_cast<const uint4*>(kt + (i * kRowsApart * pitch + my_offset));
+        c.v[i] = *reinterpret_cast<const uint4*>(vt + (i * kRowsApart * pitch + my_offset));
+      } else {
+        const uint32_t at = (uint32_t)min(row, n - 1 - key0) * pitch + (in_row ? my_chunk * 16 : 0);
+        c.k[i] = *reinterpret_cast<const uint4*>(kt + at);
+        c.v[i] = *reinterpret_cast<const uint4*>(vt + at);
+        if (key0 + row >= n) c.v[i] = make_uint4(0, 0, 0, 0);
       }
+      if (!in_row) c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
     }
   };
-  auto place = [&](Codes& c, int buf, int t) {
+  unsigned char* const my_k = smem + my_row * row_pitch<HD>() + my_chunk * 32;
+  unsigned char* const my_v = smem + 2 * kKTile + my_row * value_pitch<HD>() + my_chunk * 32;
+  auto place = [&](Codes& c, auto buf_c, int t) {
+    constexpr int buf = decltype(buf_c)::value;
     const bool partly = (t + 1) * kBlockKeys > all_see;  // a weight of 0 times a NaN code would be a NaN in rows that do not see it
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < Codes::kPer; i++) {
-      const int at = tid + i * NT, row = at / (HD / 16), chunk = at % (HD / 16);
       const bool kf = folds(c.ks[i]), vf = folds(c.vs[i]);
-      if (chunk == 0 && (row & 15) == 0) {
-        rest[buf][0][row >> 4] = kf ? 1.f : c.ks[i];
-        rest[buf][1][row >> 4] = vf ? 1.f : c.vs[i];
+      if (my_chunk == 0 && (my_row & 15) == 0) {
+        const int of16 = (my_row + i * kRowsApart) >> 4;
+        rest[buf][0][of16] = kf ? 1.f : c.ks[i];
+        rest[buf][1][of16] = vf ? 1.f : c.vs[i];
+        if (!kf || !vf) unfolded[buf] = t;
       }
       if (partly) {
         uint32_t* u = reinterpret_cast<uint32_t*>(&c.v[i]);
@@ -669,31 +717,31 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
           u[j] &= ~(is | (is - (is >> 7)));
         }
       }
-      unsigned char* kt = smem + buf * kTile + row * TL::kRowBytes;
-      unsigned char* vt = smem + (2 + buf) * kTile + row * TL::kRowBytes;
       const float kfold = kf ? c.ks[i] : 1.f, vfold = vf ? c.vs[i] : 1.f;
-      const int sk = TL::swz(row), sv = swz_v<HD>(row);
-      *reinterpret_cast<uint4*>(kt + (((2 * chunk) ^ sk) * 16)) = codes_to_bf16x8(c.k[i].x, c.k[i].y, kfold);
-      *reinterpret_cast<uint4*>(kt + (((2 * chunk + 1) ^ sk) * 16)) = codes_to_bf16x8(c.k[i].z, c.k[i].w, kfold);
-      *reinterpret_cast<uint4*>(vt + (((2 * chunk) ^ sv) * 16)) = codes_to_bf16x8(c.v[i].x, c.v[i].y, vfold);
-      *reinterpret_cast<uint4*>(vt + (((2 * chunk + 1) ^ sv) * 16)) = codes_to_bf16x8(c.v[i].z, c.v[i].w, vfold);
+      uint4* kt = reinterpret_cast<uint4*>(my_k + buf * kKTile + i * kRowsApart * row_pitch<HD>());
+      uint4* vt = reinterpret_cast<uint4*>(my_v + buf * kVTile + i * kRowsApart * value_pitch<HD>());
+      kt[0] = codes_to_bf16x8(c.k[i].x, c.k[i].y, kfold), kt[1] = codes_to_bf16x8(c.k[i].z, c.k[i].w, kfold);
+      vt[0] = codes_to_bf16x8(c.v[i].x, c.v[i].y, vfold), vt[1] = codes_to_bf16x8(c.v[i].z, c.v[i].w, vfold);
     }
     if (partly && nan) *nan_seen = 1;
   };
+  const unsigned char* const k_lane = smem + l32 * row_pitch<HD>() + hi * 16;
+  const unsigned char* const v_lane = smem + 2 * kKTile + value_base(value_pitch<HD>(), lane);
 
   f32x16 o[DB];
 #pragma unroll
   for (int j = 0; j < DB; j++) o[j] = f32x16{0};
   float m = kNoKey, l = 0.f;  // reference in base 2, this lane's sum
 
-  auto work = [&](int buf, int t) {
-    const unsigned char* ktile = smem + buf * kTile;
-    const unsigned char* vtile = smem + (2 + buf) * kTile;
-    const bool masked = (t + 1) * kBlockKeys > wave_all;
-    const float4 kr = *reinterpret_cast<const float4*>(rest[buf][0]), vr = *reinterpret_cast<const float4*>(rest[buf][1]);
-    const bool folded = __all(kr.x == 1.f && kr.y == 1.f && kr.z == 1.f && kr.w == 1.f && vr.x == 1.f && vr.y == 1.f && vr.z == 1.f && vr.w == 1.f);
+  // BUF is a compile-time constant (the loop below is unrolled by two), so that LDS addresses are loop-invariant lane offsets plus
+  // immediates.
+  auto work = [&](auto buf_c, int t) {
+    constexpr int buf = decltype(buf_c)::value;
+    const unsigned char* ktile = k_lane + buf * kKTile;
+    const unsigned char* vtile = v_lane + buf * kVTile;
+    const bool masked = (t + 1) * kBlockKeys > wave_all, folded = __builtin_amdgcn_readfirstlane(unfolded[buf]) != t;
     bf16x8 kf[KS];
-    read_frags<HD, KS>(kf, ktile, 0, l32, hi);
+    read_rows<HD, KS>(kf, ktile, 0);
 #pragma unroll
     for (int half = 0; half < 2; half++) {
       const int key0 = t * kBlockKeys + 32 * half;
@@ -703,16 +751,16 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       for (int part = PARTS - 1; part >= 0; part--)
 #pragma unroll
         for (int j = 0; j < KS; j++) mfma_step(z, kf[j], qf[part][j]);
-      if (half == 0) read_frags<HD, KS>(kf, ktile, 1, l32, hi);  // what the arithmetic below can hide
+      if (half == 0) read_rows<HD, KS>(kf, ktile, 1);  // what the arithmetic below can hide
       bf16x8 vf[DB][2];
 #pragma unroll
       for (int j = 0; j < DB; j++)
 #pragma unroll
-        for (int st = 0; st < 2; st++) vf[j][st] = read_vt_frag<HD>(vtile, half, st, j, lane);
+        for (int st = 0; st < 2; st++) vf[j][st] = read_values<HD>(vtile, half, st, j);
       if (masked || !folded) {
 #pragma unroll
         for (int i = 0; i < 16; i++) {
-          z[i] *= i < 8 ? (half ? kr.z : kr.x) : half ? kr.w : kr.y;
+          if (!folded) z[i] *= rest[buf][0][2 * half + (i >> 3)];
           if (key0 + (i >> 2) * 8 + hi * 4 + (i & 3) > last_key) z[i] = -INFINITY;
         }
       }
@@ -736,7 +784,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
            (((e[8] + e[9]) + (e[10] + e[11])) + ((e[12] + e[13]) + (e[14] + e[15])));
       if (!folded) {
 #pragma unroll
-        for (int i = 0; i < 16; i++) e[i] *= i < 8 ? (half ? vr.z : vr.x) : half ? vr.w : vr.y;
+        for (int i = 0; i < 16; i++) e[i] *= rest[buf][1][2 * half + (i >> 3)];
       }
 #pragma unroll
       for (int st = 0; st < 2; st++) {
@@ -752,22 +800,27 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
 
   {
     Codes c;
-    if (tid == 0) *nan_seen = 0;
+    if (tid == 0) *nan_seen = 0, unfolded[0] = unfolded[1] = -1;
     __syncthreads();
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
     if (first_tile < end_tile) {
       fetch(c, first_tile);
-      place(c, 0, first_tile);
+      place(c, even, first_tile);
       if (first_tile + 1 < end_tile) fetch(c, first_tile + 1);
     }
     __syncthreads();
-    for (int t = first_tile; t < end_tile; t++) {
-      const int buf = (t - first_tile) & 1;
+    auto step = [&](auto now, auto next, int t) {
       if (t + 1 < end_tile) {
-        place(c, buf ^ 1, t + 1);
+        place(c, next, t + 1);
         if (t + 2 < end_tile) fetch(c, t + 2);
       }
-      if (active && t * kBlockKeys < wave_any) work(buf, t);
+      if (active && t * kBlockKeys < wave_any) work(now, t);
       __syncthreads();
+    };
+    for (int t = first_tile; t < end_tile; t += 2) {
+      step(even, odd, t);
+      if (t + 1 < end_tile) step(odd, even, t + 1);
     }
   }
 
@@ -846,11 +899,10 @@ __global__ __launch_bounds__(256) void kv8_join_rows(Kv8Plan pl, T* __restrict__
 template <typename T, int HD, int KS, int NK, int NW>
 __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_accumulate_block(Kv8Plan pl, const T* __restrict__ q,
                                                                                                const float2* __restrict__ rows) {
-  using TL = Tile<HD>;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int PARTS = F32 ? 3 : 1, NT = NW * 64, QT = F32 ? 32 : 64;  // query rows of a tile
-  constexpr int kPart = QT * TL::kRowBytes, kTile = PARTS * kPart;
-  constexpr int kPer = QT * TL::kChunks / NT;  // 8-value chunks of a tile per thread
+  constexpr int kPart = QT * row_pitch<HD>(), kTile = PARTS * kPart, kChunks = HD / 8;
+  constexpr int kPer = QT * kChunks / NT;  // 8-value chunks of a tile per thread
   static_assert(kPer >= 1, "every thread has a chunk");
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   float(*info)[3][QT] = reinterpret_cast<float(*)[3][QT]>(smem + 2 * kTile);  // [buffer]: reference, 1 / sum, last key
@@ -889,7 +941,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   auto fetch = [&](Share& c, int tile) {
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
-      const int at = tid + i * NT, r = tile * QT + at / TL::kChunks, column = at % TL::kChunks * 8;
+      const int at = tid + i * NT, r = tile * QT + at / kChunks, column = at % kChunks * 8;
       int g, t;
       head_and_token(pl.p, pl.inv_p, min(r, pl.R - 1), g, t);
       const T* from = q + b * pl.qsb + (int64_t)(h * pl.G + g) * pl.qsh + (int64_t)t * pl.qst + column;
@@ -917,8 +969,8 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     unsigned char* tile = smem + buf * kTile;
 #pragma unroll
     for (int i = 0; i < kPer; i++) {
-      const int at = tid + i * NT, r = at / TL::kChunks, chunk = at % TL::kChunks;
-      uint4* to = reinterpret_cast<uint4*>(tile + r * TL::kRowBytes + ((chunk ^ TL::swz(r)) * 16));
+      const int at = tid + i * NT, r = at / kChunks, chunk = at % kChunks;
+      uint4* to = reinterpret_cast<uint4*>(tile + r * row_pitch<HD>() + chunk * 16);
       if constexpr (F32) {
         bf16x8 parts[3];
         cut_row8(parts, c.v[i], true);
@@ -951,7 +1003,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       if (row0 >= pl.R || key0 >= most) continue;
       bf16x8 qf[PARTS][KS];
 #pragma unroll
-      for (int p = 0; p < PARTS; p++) read_frags<HD, KS>(qf[p], smem + buf * kTile + p * kPart, half, l32, hi);
+      for (int p = 0; p < PARTS; p++) read_rows<HD, KS>(qf[p], smem + buf * kTile + p * kPart + l32 * row_pitch<HD>() + hi * 16, half);
       float m[16], inv[16];  // of the lane's rows 8 (i / 4) + 4 hi + i % 4
 #pragma unroll
       for (int i = 0; i < 4; i++) {
@@ -1091,7 +1143,7 @@ hipError_t launch_block(const Kv8Plan& pl, const T* q, T* out, float* lse, void*
   const BlockRoom room = block_room(pl, workspace, &bytes);
   const int heads = pl.nb * pl.Hkv, n_rb = (pl.R + 32 * NW - 1) / (32 * NW);
   hipError_t e = launch_with_lds(kv8_attention_block<T, HD, KS, DB, NW>, dim3(8 * n_rb, (heads * room.splits + 7) / 8), NW * 64,
-                                 4 * kBlockKeys * Tile<HD>::kRowBytes + 128, stream, pl, q, out, lse, room);
+                                 block_tiles_bytes<HD>() + 128, stream, pl, q, out, lse, room);
   if (e != hipSuccess) return e;
   if (room.splits > 1) {
     const size_t threads = (size_t)heads * pl.R * (pl.d / 4);
@@ -1101,7 +1153,7 @@ hipError_t launch_block(const Kv8Plan& pl, const T* q, T* out, float* lse, void*
   }
   if (!pl.accumulate) return hipSuccess;
   constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = sizeof(T) == 4 ? 32 : 64, NK = HD == 256 ? 1 : 2;
-  constexpr size_t lds = 2 * PARTS * QT * Tile<HD>::kRowBytes + 2 * 3 * QT * sizeof(float);
+  constexpr size_t lds = 2 * PARTS * QT * row_pitch<HD>() + 2 * 3 * QT * sizeof(float);
   const int keys = 32 * NK * 4;
   return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + keys - 1) / keys, heads), 256, lds,
                          stream, pl, q, room.rows);
