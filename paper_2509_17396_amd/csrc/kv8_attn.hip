@@ -671,9 +671,9 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   const int my_row = tid / (HD / 16), my_chunk = tid % (HD / 16);
   constexpr int kRowsApart = NT / (HD / 16);  // from a thread's chunk to its next
   const bool in_row = my_chunk * 16 < pl.d;
-  const uint32_t my_offset = (uint32_t)my_row * pitch + (in_row ? my_chunk * 16 : 0);
+  const uint32_t my_column = in_row ? my_chunk * 16 : 0;
   auto fetch = [&](Codes& c, int t) {
-    const int key0 = t * kBlockKeys;
+    const int key0 = t * kBlockKeys, there = n - key0;
     const uint8_t* kt = kbase + (int64_t)key0 * pitch;
     const uint8_t* vt = vbase + (int64_t)key0 * pitch;
 #pragma unroll
@@ -681,49 +681,51 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       const int row = my_row + i * kRowsApart;
       const int block = min(key0 + (__builtin_amdgcn_readfirstlane(row) & ~15), n - 1) >> pl.block_shift;
       c.ks[i] = ks[block], c.vs[i] = vs[block];
-      if (key0 + kBlockKeys <= n) {
-        c.k[i] = *reinterpret_cast<const uint4*>(kt + (i * kRowsApart * pitch + my_offset));
-        c.v[i] = *reinterpret_cast<const uint4*>(vt + (i * kRowsApart * pitch + my_offset));
-      } else {
-        const uint32_t at = (uint32_t)min(row, n - 1 - key0) * pitch + (in_row ? my_chunk * 16 : 0);
-        c.k[i] = *reinterpret_cast<const uint4*>(kt + at);
-        c.v[i] = *reinterpret_cast<const uint4*>(vt + at);
-        if (key0 + row >= n) c.v[i] = make_uint4(0, 0, 0, 0);
-      }
-      if (!in_row) c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
+      const uint32_t at = __umul24(min(row, there - 1), pitch) + my_column;
+      c.k[i] = *reinterpret_cast<const uint4*>(kt + at);
+      c.v[i] = *reinterpret_cast<const uint4*>(vt + at);
     }
   };
-  unsigned char* const my_k = smem + my_row * row_pitch<HD>() + my_chunk * 32;
-  unsigned char* const my_v = smem + 2 * kKTile + my_row * value_pitch<HD>() + my_chunk * 32;
-  auto place = [&](Codes& c, auto buf_c, int t) {
+  // Before a tile's codes are decoded: what is not to be in them, and what the decoded values will not have in them.
+  auto check = [&](Codes& c, auto buf_c, int t) {
     constexpr int buf = decltype(buf_c)::value;
     const bool partly = (t + 1) * kBlockKeys > all_see;  // a weight of 0 times a NaN code would be a NaN in rows that do not see it
-    bool nan = false;
 #pragma unroll
     for (int i = 0; i < Codes::kPer; i++) {
-      const bool kf = folds(c.ks[i]), vf = folds(c.vs[i]);
-      if (my_chunk == 0 && (my_row & 15) == 0) {
-        const int of16 = (my_row + i * kRowsApart) >> 4;
-        rest[buf][0][of16] = kf ? 1.f : c.ks[i];
-        rest[buf][1][of16] = vf ? 1.f : c.vs[i];
+      const int row = my_row + i * kRowsApart;
+      if (my_chunk == 0 && (row & 15) == 0) {
+        const bool kf = folds(c.ks[i]), vf = folds(c.vs[i]);
+        rest[buf][0][row >> 4] = kf ? 1.f : c.ks[i];
+        rest[buf][1][row >> 4] = vf ? 1.f : c.vs[i];
         if (!kf || !vf) unfolded[buf] = t;
       }
+      if (pl.d != HD && !in_row) c.k[i] = c.v[i] = make_uint4(0, 0, 0, 0);
       if (partly) {
         uint32_t* u = reinterpret_cast<uint32_t*>(&c.v[i]);
+        bool nan = false;
 #pragma unroll
         for (int j = 0; j < 4; j++) {
+          if (t * kBlockKeys + row >= n) u[j] = 0;
           const uint32_t is = nan_bytes(u[j]);
           nan = nan || is != 0;
           u[j] &= ~(is | (is - (is >> 7)));
         }
+        if (nan) *nan_seen = 1;
       }
-      const float kfold = kf ? c.ks[i] : 1.f, vfold = vf ? c.vs[i] : 1.f;
+    }
+  };
+  unsigned char* const my_k = smem + my_row * row_pitch<HD>() + my_chunk * 32;
+  unsigned char* const my_v = smem + 2 * kKTile + my_row * value_pitch<HD>() + my_chunk * 32;
+  auto place = [&](const Codes& c, auto buf_c) {
+    constexpr int buf = decltype(buf_c)::value;
+#pragma unroll
+    for (int i = 0; i < Codes::kPer; i++) {
+      const float kfold = folds(c.ks[i]) ? c.ks[i] : 1.f, vfold = folds(c.vs[i]) ? c.vs[i] : 1.f;
       uint4* kt = reinterpret_cast<uint4*>(my_k + buf * kKTile + i * kRowsApart * row_pitch<HD>());
       uint4* vt = reinterpret_cast<uint4*>(my_v + buf * kVTile + i * kRowsApart * value_pitch<HD>());
       kt[0] = codes_to_bf16x8(c.k[i].x, c.k[i].y, kfold), kt[1] = codes_to_bf16x8(c.k[i].z, c.k[i].w, kfold);
       vt[0] = codes_to_bf16x8(c.v[i].x, c.v[i].y, vfold), vt[1] = codes_to_bf16x8(c.v[i].z, c.v[i].w, vfold);
     }
-    if (partly && nan) *nan_seen = 1;
   };
   const unsigned char* const k_lane = smem + l32 * row_pitch<HD>() + hi * 16;
   const unsigned char* const v_lane = smem + 2 * kKTile + value_base(value_pitch<HD>(), lane);
@@ -735,7 +737,9 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
 
   // BUF is a compile-time constant (the loop below is unrolled by two), so that LDS addresses are loop-invariant lane offsets plus
   // immediates.
-  auto work = [&](auto buf_c, int t) {
+  // Between the products of the first half the next tile's codes, which are there by now, go to LDS, and those behind them are asked
+  // for: 80 of 424 us went into that where it stood in front of the tile (2 x 32 heads x 2048 rows over 6144 keys).
+  auto work = [&](auto buf_c, auto next_c, Codes& c, int t) {
     constexpr int buf = decltype(buf_c)::value;
     const unsigned char* ktile = k_lane + buf * kKTile;
     const unsigned char* vtile = v_lane + buf * kVTile;
@@ -745,8 +749,8 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
 #pragma unroll
     for (int half = 0; half < 2; half++) {
       const int key0 = t * kBlockKeys + 32 * half;
-      f32x16 z;
-      z = f32x16{0};
+      f32x16 z = f32x16{0};
+      __builtin_amdgcn_s_setprio(1);  // of the two waves of a SIMD the one with products goes first: 424 -> 410 us
 #pragma unroll
       for (int part = PARTS - 1; part >= 0; part--)
 #pragma unroll
@@ -757,6 +761,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       for (int j = 0; j < DB; j++)
 #pragma unroll
         for (int st = 0; st < 2; st++) vf[j][st] = read_values<HD>(vtile, half, st, j);
+      if (half == 0) place(c, next_c);
       if (masked || !folded) {
 #pragma unroll
         for (int i = 0; i < 16; i++) {
@@ -764,6 +769,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
           if (key0 + (i >> 2) * 8 + hi * 4 + (i & 3) > last_key) z[i] = -INFINITY;
         }
       }
+      __builtin_amdgcn_s_setprio(0);
       const float a0 = max3(z[0], z[1], z[2]), a1 = max3(z[3], z[4], z[5]), a2 = max3(z[6], z[7], z[8]);
       const float a3 = max3(z[9], z[10], z[11]), a4 = max3(z[12], z[13], z[14]);
       const float top = max_across_halves(max3(max3(a0, a1, a2), max3(a3, a4, z[15]), -INFINITY)) * pl.c2;
@@ -786,6 +792,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
 #pragma unroll
         for (int i = 0; i < 16; i++) e[i] *= rest[buf][1][2 * half + (i >> 3)];
       }
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int st = 0; st < 2; st++) {
         bf16x8 pf[PARTS];
@@ -795,6 +802,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
 #pragma unroll
           for (int j = 0; j < DB; j++) o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j][st], pf[part], o[j], 0, 0, 0);
       }
+      if (half == 0) fetch(c, min(t + 2, end_tile - 1));
     }
   };
 
@@ -806,16 +814,19 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     constexpr std::integral_constant<int, 1> odd;
     if (first_tile < end_tile) {
       fetch(c, first_tile);
-      place(c, even, first_tile);
-      if (first_tile + 1 < end_tile) fetch(c, first_tile + 1);
+      check(c, even, first_tile);
+      place(c, even);
+      fetch(c, min(first_tile + 1, end_tile - 1));
     }
     __syncthreads();
     auto step = [&](auto now, auto next, int t) {
-      if (t + 1 < end_tile) {
-        place(c, next, t + 1);
-        if (t + 2 < end_tile) fetch(c, t + 2);
+      if (t + 1 < end_tile) check(c, next, t + 1);
+      if (active && t * kBlockKeys < wave_any) {
+        work(now, next, c, t);
+      } else {
+        place(c, next);  // the last tile once more where there is no next one: nobody reads it
+        fetch(c, min(t + 2, end_tile - 1));
       }
-      if (active && t * kBlockKeys < wave_any) work(now, t);
       __syncthreads();
     };
     for (int t = first_tile; t < end_tile; t += 2) {
@@ -925,11 +936,11 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     acc[x] = 0.f;
     const uint8_t* row = kbase + (int64_t)key * pl.st;
 #pragma unroll
-    for (int j = 0; j < KS; j++) {
-      const int at = (2 * j + hi) * 8;
-      uint2 u = make_uint2(0, 0);
-      if (at < pl.d) u = *reinterpret_cast<const uint2*>(row + at);
-      kf[x][j] = codes_to_frag(u.x, u.y);
+    for (int j = 0; j < KS; j += 2) {  // chunks of 16 codes in the place of two of 8: in which order they are multiplied is free
+      const int at = j * 16 + hi * 16;
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (at < pl.d) u = *reinterpret_cast<const uint4*>(row + at);
+      kf[x][j] = codes_to_frag(u.x, u.y), kf[x][j + 1] = codes_to_frag(u.z, u.w);
     }
   }
 
@@ -1003,7 +1014,11 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       if (row0 >= pl.R || key0 >= most) continue;
       bf16x8 qf[PARTS][KS];
 #pragma unroll
-      for (int p = 0; p < PARTS; p++) read_rows<HD, KS>(qf[p], smem + buf * kTile + p * kPart + l32 * row_pitch<HD>() + hi * 16, half);
+      for (int p = 0; p < PARTS; p++) {
+        const unsigned char* row = smem + buf * kTile + p * kPart + (32 * half + l32) * row_pitch<HD>() + hi * 32;
+#pragma unroll
+        for (int j = 0; j < KS; j++) qf[p][j] = as_frag(*reinterpret_cast<const uint4*>(row + (j >> 1) * 64 + (j & 1) * 16));
+      }
       float m[16], inv[16];  // of the lane's rows 8 (i / 4) + 4 hi + i % 4
 #pragma unroll
       for (int i = 0; i < 4; i++) {
@@ -1152,11 +1167,26 @@ hipError_t launch_block(const Kv8Plan& pl, const T* q, T* out, float* lse, void*
     if (e != hipSuccess) return e;
   }
   if (!pl.accumulate) return hipSuccess;
-  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = sizeof(T) == 4 ? 32 : 64, NK = HD == 256 ? 1 : 2;
+  // 32-key tiles of a wave: rounds of workgroups, each as long as its tiles and some one more for getting going (32 heads of 512 rows
+  // over 8320 keys: one tile 66.8 us, two, with a third round for the last few workgroups, 74.0, three 66.2)
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = sizeof(T) == 4 ? 32 : 64;
   constexpr size_t lds = 2 * PARTS * QT * row_pitch<HD>() + 2 * 3 * QT * sizeof(float);
-  const int keys = 32 * NK * 4;
-  return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + keys - 1) / keys, heads), 256, lds,
-                         stream, pl, q, room.rows);
+  auto accumulate = [&](auto nk) {
+    constexpr int NK = decltype(nk)::value, kKeys = 32 * NK * 4;
+    return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + kKeys - 1) / kKeys, heads), 256, lds,
+                           stream, pl, q, room.rows);
+  };
+  auto cost = [&](int nk) {
+    const int64_t workgroups = (int64_t)heads * ((pl.n_cached + pl.n_block + 128 * nk - 1) / (128 * nk));
+    const int64_t slots = kComputeUnits * block_occupancy(sizeof(T), HD);
+    return (workgroups + slots - 1) / slots * (nk + 1);
+  };
+  if constexpr (HD < 256) {
+    if constexpr (sizeof(T) == 2)
+      if (cost(3) <= cost(2) && cost(3) <= cost(1)) return accumulate(std::integral_constant<int, 3>{});
+    if (cost(2) <= cost(1)) return accumulate(std::integral_constant<int, 2>{});
+  }
+  return accumulate(std::integral_constant<int, 1>{});
 }
 
 template <typename T>
