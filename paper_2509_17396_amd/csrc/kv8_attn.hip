@@ -381,6 +381,7 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
     // two steps' rows on their way: one is asked for as soon as its registers are free
     Step<NCH> one, two;
     const std::true_type in;
+    const std::false_type any;
     const int inside_end = min(end, all_see / kTokenKeys);
     int tile = split * per_split + wave;
     if (tile < inside_end) load(in, one, tile);
@@ -396,8 +397,8 @@ __global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * 
       if (tile + 3 * kTokenWaves < inside_end) load(in, two, tile + 3 * kTokenWaves);
     }
     for (; tile < end; tile += kTokenWaves) {  // the last ones
-      load(std::false_type{}, one, tile);
-      work(std::false_type{}, one, tile);
+      load(any, one, tile);
+      work(any, one, tile);
     }
   }
 
@@ -467,6 +468,15 @@ __global__ __launch_bounds__(256) void kv8_join_tokens(Kv8Plan pl, T* __restrict
   const bool is_out = (int)blockIdx.x < out_blocks;
   const int key = ((int)blockIdx.x - out_blocks) * 1024 + tid * 4;
   if (!is_out && key - tid * 4 >= n) return;
+  // the first rows' logits are on their way while the sums are put together
+  constexpr int kEarly = 4;
+  const float* logits = room.logits + (size_t)bh * pl.R * room.logit_pitch + key;
+  float4 early[kEarly];
+  if (!is_out && key < n) {
+#pragma unroll
+    for (int i = 0; i < kEarly; i++)
+      if (i < pl.R) early[i] = *reinterpret_cast<const float4*>(logits + (size_t)i * room.logit_pitch);
+  }
   {  // eight lanes to a row
     const int row = tid >> 3;
     float mn = kNoKey, sum = 0.f;
@@ -512,12 +522,15 @@ __global__ __launch_bounds__(256) void kv8_join_tokens(Kv8Plan pl, T* __restrict
   }
   if (key >= n) return;
   float w[4] = {0, 0, 0, 0};
-  for (int row = 0; row < pl.R; row++) {
-    const float4 x = *reinterpret_cast<const float4*>(room.logits + ((size_t)bh * pl.R + row) * room.logit_pitch + key);
+  auto add = [&](const float4& x, int row) {
     const float2 ml = row_ml[row];
-    if (ml.y == 0.f) continue;
+    if (ml.y == 0.f) return;
     w[0] += ex2(x.x - ml.x) * ml.y, w[1] += ex2(x.y - ml.x) * ml.y, w[2] += ex2(x.z - ml.x) * ml.y, w[3] += ex2(x.w - ml.x) * ml.y;
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < kEarly; i++)
+    if (i < pl.R) add(early[i], i);
+  for (int row = kEarly; row < pl.R; row++) add(*reinterpret_cast<const float4*>(logits + (size_t)row * room.logit_pitch), row);
   float* to = pl.weight + b * pl.rsb + h * pl.rsh + key;
 #pragma unroll
   for (int i = 0; i < 4; i++)
