@@ -1,4 +1,15 @@
-// Attention over the 8-bit cache (epicache_kv8_attention).
+// Attention over the 8-bit cache (epicache_kv8_attention): O_t = sum_i softmax_i(scale q_t . k_i) v_i and the log of the sum, k_i and v_i
+// being e4m3 codes times their block's scale; with `accumulate` the softmax weights that a key receives are added to its own.
+//
+// An e4m3 code is a bf16 value exactly, so all products run on the bf16 matrix cores on decoded codes; scales are multiplied with the
+// logits and the weights in fp32 (or, powers of two, folded into the decoded value, which stays exact).  fp32 queries and weights are cut
+// into bf16 parts whose sum they are: three for fp32 outputs, two for the weights of few rows, one (rounded to bf16, 2^-8 of a weight, as
+// the output itself is) for the weights of many bf16 rows, where a second part would cost half as many products again.
+// The softmax is taken in one pass with a running reference and sum per row, in fp32 and base 2.
+//
+// Few rows per KV head (a decoding step: up to 32, 16 for head_dim above 128) are bound by the codes' way from memory: kv8_attention_tokens,
+// 16 x 8 heads of 24576 rows 128 us, 6.3 TB/s.  Many rows are bound by the products and the softmax between them: kv8_attention_block, 2 x 32
+// heads of 2048 rows over 6144 keys 405 us, 850 TFLOP/s.
 #include <hip/hip_bf16.h>
 
 #include <algorithm>
@@ -11,6 +22,14 @@ namespace epicache {
 namespace {
 
 // ---- Few query rows per KV head (decoding): every wave streams its own keys through registers.
+//
+// Steps of 32 keys go from memory to the matrix cores without LDS.  S^T = K Q^T with 16x16x32 products: a lane holds one query and the keys
+// 4 g + i and 16 + 4 g + i of the step, which is how O^T += V^T P^T wants its weights.  V^T wants 8 keys of one column in a lane, so a
+// lane fetches its columns of those 8 rows and pairs the bytes of neighbouring keys with permutations, two bytes to an instruction.
+// The order of the contraction over head_dim is free, so a lane's 16-byte chunks of K need no shuffling either.
+// What it took: rows' tiles handled apart from the last ones and two steps in flight without spills 221 -> 147 us (16 x 8 heads of 24576
+// rows), codes read past the caches 139 -> 128 us.  The workgroups of a head each leave their reference, sum and output, and where
+// weights are accumulated the logits (a few bytes per key and query beside 256 of codes); kv8_join_tokens puts them together.
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
@@ -540,19 +559,21 @@ __global__ __launch_bounds__(256) void kv8_join_tokens(Kv8Plan pl, T* __restrict
 // ---- Many query rows per KV head (patches, prefilled blocks): tiles of keys through LDS, shared by the waves of a workgroup.
 //
 // A wave owns 32 query rows.  Tiles of 64 rows of K and V come from memory as codes, one tile ahead, are decoded to bf16 (exactly,
-// with their scale where it is a power of two) by whoever fetched them and lie in LDS double
-// buffered.  Per 32 keys: S^T = K Q^T, an online softmax, O^T += V^T P^T.
+// with their scale where it is a power of two) by whoever fetched them, once per workgroup, and lie in LDS double buffered.  Per 32 keys: S^T = K Q^T, an online softmax, O^T += V^T P^T.
 
 struct BlockRoom {
   int splits, split_tiles;  // workgroups that share the keys of a row, and the tiles of each
   float2* rows;             // [heads][R]: reference and 1 / sum, where weights are accumulated
   float2* stats;            // [heads][splits][R], where there are several: reference and sum
   float* records;           // [heads][splits][R][d]: outputs before the division
+  int row_splits, pitch;    // workgroups that share the rows of a key, where weights are accumulated
+  float* sums;              // [heads][row_splits][pitch], where there are several: what each has of a key's weight
 };
 
 constexpr int kBlockKeys = 64;
 
-// Waves of a workgroup.  The fewer rows, the more of them only help with the tiles.
+// Waves of a workgroup.  The fewer rows, the more of them only help with the tiles.  Eight share one tile where it has a chunk for each
+// of their threads (head_dim above 64).
 int block_waves(const Kv8Plan& pl) { return pl.R > 128 && pl.d > 64 && pl.d <= 128 && pl.dtype == EPICACHE_DTYPE_BF16 ? 8 : 4; }
 
 __device__ __forceinline__ bool folds(float scale) {  // into the exponent of a decoded value
@@ -917,14 +938,15 @@ __global__ __launch_bounds__(256) void kv8_join_rows(Kv8Plan pl, T* __restrict__
   }
 }
 
+constexpr int accumulate_rows(bool f32) { return f32 ? 32 : 64; }  // query rows of a tile
+
 // weight += the softmax weights of many rows: the product with K once more, now with the keys in registers and the query rows
 // through LDS, so that every key's sum has one owner and one order.  A wave has 32 NK keys, a lane one column of each 32 and half
 // of its rows: a key's scale and its sum are the lane's own, what belongs to a row comes from LDS.
 template <typename T, int HD, int KS, int NK, int NW>
-__global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_accumulate_block(Kv8Plan pl, const T* __restrict__ q,
-                                                                                               const float2* __restrict__ rows) {
+__global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_accumulate_block(Kv8Plan pl, const T* __restrict__ q, BlockRoom room) {
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int PARTS = F32 ? 3 : 1, NT = NW * 64, QT = F32 ? 32 : 64;  // query rows of a tile
+  constexpr int PARTS = F32 ? 3 : 1, NT = NW * 64, QT = accumulate_rows(F32);
   constexpr int kPart = QT * row_pitch<HD>(), kTile = PARTS * kPart, kChunks = HD / 8;
   constexpr int kPer = QT * kChunks / NT;  // 8-value chunks of a tile per thread
   static_assert(kPer >= 1, "every thread has a chunk");
@@ -982,7 +1004,7 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
       c.ml = make_float2(0.f, 0.f);
       int g = 0, t = 0;
       if (r < pl.R) {
-        c.ml = rows[(size_t)bh * pl.R + r];
+        c.ml = room.rows[(size_t)bh * pl.R + r];
         head_and_token(pl.p, pl.inv_p, r, g, t);
       }
       if (c.ml.y == 0.f) c.ml.x = INFINITY;  // a row without weights: exponentials of -inf, whatever its logits
@@ -1007,14 +1029,15 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
     if (tid < QT) info[buf][0][tid] = c.ml.x, info[buf][1][tid] = c.ml.y, info[buf][2][tid] = __int_as_float(c.last);
   };
 
-  const int tiles = (pl.R + QT - 1) / QT;
+  const int all_tiles = (pl.R + QT - 1) / QT, per_split = (all_tiles + room.row_splits - 1) / room.row_splits;
+  const int first_tile = blockIdx.z * per_split, tiles = min(all_tiles, first_tile + per_split);
   Share c;
-  fetch(c, 0);
+  fetch(c, first_tile);
   place(c, 0);
-  if (tiles > 1) fetch(c, 1);
+  if (first_tile + 1 < tiles) fetch(c, first_tile + 1);
   __syncthreads();
-  for (int t = 0; t < tiles; t++) {
-    const int buf = t & 1;
+  for (int t = first_tile; t < tiles; t++) {
+    const int buf = (t - first_tile) & 1;
     if (t + 1 < tiles) {
       place(c, buf ^ 1);
       if (t + 2 < tiles) fetch(c, t + 2);
@@ -1067,8 +1090,19 @@ __global__ __launch_bounds__(NW * 64, block_occupancy(sizeof(T), HD)) void kv8_a
   for (int x = 0; x < NK; x++) {
     const float sum = acc[x] + __shfl_xor(acc[x], 32);
     const int key = key0 + 32 * x + l32;
-    if (hi == 0 && key < n) weight[key] += sum;
+    if (hi != 0 || key >= n) continue;
+    if (room.row_splits == 1) weight[key] += sum;
+    else room.sums[((size_t)bh * room.row_splits + blockIdx.z) * room.pitch + key] = sum;
   }
+}
+
+// weight += the row splits' sums, in their order.
+__global__ __launch_bounds__(256) void kv8_add_sums(Kv8Plan pl, BlockRoom room) {
+  const int bh = blockIdx.y, b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv, key = blockIdx.x * 256 + threadIdx.x;
+  if (key >= kv8_old_rows(pl, bh) + pl.n_block) return;
+  float sum = 0.f;
+  for (int i = 0; i < room.row_splits; i++) sum += room.sums[((size_t)bh * room.row_splits + i) * room.pitch + key];
+  pl.weight[b * pl.rsb + h * pl.rsh + key] += sum;
 }
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -1077,7 +1111,8 @@ size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 TokenRoom token_room(const Kv8Plan& pl, void* workspace, size_t* bytes) {
   const int64_t heads = (int64_t)pl.nb * pl.Hkv;
   const int tiles = (pl.n_cached + pl.n_block + kTokenKeys - 1) / kTokenKeys;
-  // a round of resident workgroups, each with two steps a wave at least
+  // A round of resident workgroups, each with two steps a wave at least; two rounds where the steps are many, so that the last workgroups
+  // to end are shorter (64 x 4 heads of 8193 keys: one 156 us, two 150; 96 heads of up to 2501 keys: one 18.3, more 23.2).
   const int64_t slots = kComputeUnits * token_occupancy(pl.dtype == EPICACHE_DTYPE_F32 ? 4 : 2, (pl.d + 63) / 64 * ((pl.R + 15) / 16));
   int64_t splits = slots / heads;
   if (splits > 0 && tiles / splits >= 16 * kTokenWaves) splits *= 2;
@@ -1138,7 +1173,7 @@ BlockRoom block_room(const Kv8Plan& pl, void* workspace, size_t* bytes) {
   splits = std::max<int64_t>(1, std::min<int64_t>({splits, tiles / 4, kMostSplits}));
   const int split_tiles = (tiles + (int)splits - 1) / (int)splits;
   splits = (tiles + split_tiles - 1) / split_tiles;
-  BlockRoom room = {(int)splits, split_tiles, nullptr, nullptr, nullptr};
+  BlockRoom room = {(int)splits, split_tiles, nullptr, nullptr, nullptr, 1, (tiles * kBlockKeys + 127) / 128 * 128, nullptr};
   char* ws = static_cast<char*>(workspace);
   size_t at = 0;
   auto take = [&](size_t n) {
@@ -1150,6 +1185,17 @@ BlockRoom block_room(const Kv8Plan& pl, void* workspace, size_t* bytes) {
   if (splits > 1) {
     room.stats = reinterpret_cast<float2*>(take((size_t)heads * splits * pl.R * sizeof(float2)));
     room.records = take((size_t)heads * splits * pl.R * pl.d * sizeof(float));
+  }
+  if (pl.accumulate) {
+    // Few heads and keys and many rows: the rows are shared too, two tiles of them at least to a workgroup (24 heads of 1368 rows over some
+    // 1400 keys: 132 us with one workgroup to 128 keys).
+    const bool f32 = pl.dtype == EPICACHE_DTYPE_F32;
+    const int row_tiles = (pl.R + accumulate_rows(f32) - 1) / accumulate_rows(f32);
+    const int64_t workgroups = heads * (room.pitch / 128), resident = kComputeUnits * block_occupancy(f32 ? 4 : 2, pl.d <= 128 ? 128 : 256);
+    const int wanted = (int)std::max<int64_t>(1, std::min<int64_t>(resident / workgroups, row_tiles / 2));
+    const int per_split = (row_tiles + wanted - 1) / wanted;
+    room.row_splits = (row_tiles + per_split - 1) / per_split;
+    if (room.row_splits > 1) room.sums = take((size_t)heads * room.row_splits * room.pitch * sizeof(float));
   }
   *bytes = at;
   return room;
@@ -1182,13 +1228,19 @@ hipError_t launch_block(const Kv8Plan& pl, const T* q, T* out, float* lse, void*
   if (!pl.accumulate) return hipSuccess;
   // 32-key tiles of a wave: rounds of workgroups, each as long as its tiles and some one more for getting going (32 heads of 512 rows
   // over 8320 keys: one tile 66.8 us, two, with a third round for the last few workgroups, 74.0, three 66.2)
-  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = sizeof(T) == 4 ? 32 : 64;
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, QT = accumulate_rows(sizeof(T) == 4);
   constexpr size_t lds = 2 * PARTS * QT * row_pitch<HD>() + 2 * 3 * QT * sizeof(float);
   auto accumulate = [&](auto nk) {
     constexpr int NK = decltype(nk)::value, kKeys = 32 * NK * 4;
-    return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + kKeys - 1) / kKeys, heads), 256, lds,
-                           stream, pl, q, room.rows);
+    return launch_with_lds(kv8_accumulate_block<T, HD, KS, NK, 4>, dim3((pl.n_cached + pl.n_block + kKeys - 1) / kKeys, heads, room.row_splits),
+                           256, lds, stream, pl, q, room);
   };
+  if (room.row_splits > 1) {
+    e = accumulate(std::integral_constant<int, 1>{});
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kv8_add_sums, dim3((pl.n_cached + pl.n_block + 255) / 256, heads), dim3(256), 0, stream, pl, room);
+    return hipGetLastError();
+  }
   auto cost = [&](int nk) {
     const int64_t workgroups = (int64_t)heads * ((pl.n_cached + pl.n_block + 128 * nk - 1) / (128 * nk));
     const int64_t slots = kComputeUnits * block_occupancy(sizeof(T), HD);
@@ -1212,6 +1264,7 @@ hipError_t launch_blocks(const Kv8Plan& pl, const T* q, T* out, float* lse, void
   };
   using std::integral_constant;
   if (pl.d <= 64) return waves(integral_constant<int, 64>{}, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  if (pl.d <= 96) return waves(integral_constant<int, 128>{}, integral_constant<int, 6>{}, integral_constant<int, 3>{});
   if (pl.d <= 128) return waves(integral_constant<int, 128>{}, integral_constant<int, 8>{}, integral_constant<int, 4>{});
   if (pl.d <= 192) return waves(integral_constant<int, 256>{}, integral_constant<int, 12>{}, integral_constant<int, 6>{});
   return waves(integral_constant<int, 256>{}, integral_constant<int, 16>{}, integral_constant<int, 8>{});
