@@ -405,8 +405,9 @@ EPICACHE_API int epicache_layer_budgets(const double* sensitivity, int32_t n_lay
  * n_cached + n_block <= capacity.  What lies behind them is neither read nor written.
  * The struct is read on the host during the call; the arrays are DEVICE memory, 16-byte aligned, the codes' strides
  * multiples of 16.  Each call checks the fields of `params` that it names, and n_batch, n_q_heads, n_kv_heads, head_dim
- * (here a multiple of 16, 16..256), n_cached, n_block, dtype; `reduce` is not used.  Same conventions as above: a call enqueues
- * on `hip_stream`, of the current device, and can be captured. */
+ * (here a multiple of 16, 16..256), n_cached, n_block, dtype; `reduce` is not used.  capacity <= 2^24, stride_t <= 2^20.  Same
+ * conventions as above: a call enqueues on `hip_stream`, of the current device, and can be captured; calls that use the same
+ * cache or workspace must be ordered by the caller. */
 typedef struct epicache_kv8 {
   uint32_t struct_size;   /* sizeof(epicache_kv8), checked                                            */
   int32_t block_tokens;   /* rows that share a scale: 16, 32, 64 or 128                                */
@@ -446,6 +447,7 @@ EPICACHE_API int epicache_kv8_append(const epicache_params* params, const epicac
  * A query without a row, or whose logits are all -inf, gets out = 0 and lse = -inf and adds nothing.
  * In: q [n_batch, n_q_heads, patch_len, head_dim] (dtype, strides q_stride_*).  Out, dense: out as q, in dtype; lse_out float32.
  * Products of the decoded values on the matrix cores, sums and exponentials in fp32; logits above -1e30.
+ * patch_len * (n_q_heads / n_kv_heads) <= 2^20, n_batch * n_q_heads * patch_len < 2^31.
  * Uses of params: patch_len, softmax_scale, causal_patch, q_stride_*. */
 EPICACHE_API int epicache_kv8_attention(const epicache_params* params, const epicache_kv8* cache, const void* q,
                                         const int32_t* n_ctx_opt, int32_t accumulate, void* out, float* lse_out,

@@ -421,6 +421,8 @@ def make_kv8(k, v, k_scale, v_scale, block_tokens: int, weight=None, position=No
             (k_scale.shape[2] == 1 or k_scale.stride(2) == 1) and
             all(t is None or (t.shape == (nb, H, C) and t.stride() == rows.stride() and (C == 1 or t.stride(2) == 1)) for t in pair)):
         raise ValueError("make_kv8: shapes or strides do not belong together")
+    if len({t.device for t in (k, v, k_scale, v_scale, *pair) if t is not None}) != 1:
+        raise ValueError("make_kv8: the tensors lie on different devices")
     row_strides = (0, 0) if rows is None else rows.stride()[:2]
     kv8 = Kv8(ctypes.sizeof(Kv8), block_tokens, C, 0, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
               None if weight is None else weight.data_ptr(), None if position is None else position.data_ptr(), *k.stride()[:3],

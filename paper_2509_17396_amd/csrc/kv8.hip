@@ -142,7 +142,7 @@ __device__ __forceinline__ uint32_t evict_key(float weight, int position, int la
   return max(min(order_key(weight), 0xff800001u), 1u);
 }
 
-// The largest magnitude among 16 codes that are numbers, as a code, and whether there are others.
+// The largest magnitude among those of 16 codes that are numbers, as a code.
 __device__ __forceinline__ uint32_t largest_code(uint4 u) {
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
   typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;

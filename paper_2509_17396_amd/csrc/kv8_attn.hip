@@ -193,13 +193,13 @@ __device__ __forceinline__ void not_numbers(Step<NCH>& s, f32x4 (&acc)[NR][4 * N
   }
 }
 
-// EXACT: d = 64 NCH; a lane's columns of V are then 4 NCH neighbouring ones, else 4 of every 64.
-// Waves per SIMD that the registers are cut for.
+// Waves per SIMD that the registers are cut for: as many as leave the hot loop without spills.
 constexpr int token_occupancy(size_t elem, int chunks) { return chunks <= 1 ? 3 : chunks <= (elem == 4 ? 2 : 3) ? 2 : 1; }
 
+// EXACT: d = 64 NCH; a lane's columns of V are then 4 NCH neighbouring ones, else 4 of every 64.  A wave has 16 NR rows.
 template <typename T, int NCH, bool EXACT, int NR>
-__global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * NR)) void kv8_attention_tokens(Kv8Plan pl, const T* __restrict__ q, T* __restrict__ out,
-                                                                        float* __restrict__ lse, TokenRoom room) {
+__global__ __launch_bounds__(kTokenWaves * 64, token_occupancy(sizeof(T), NCH * NR)) void kv8_attention_tokens(
+    Kv8Plan pl, const T* __restrict__ q, T* __restrict__ out, float* __restrict__ lse, TokenRoom room) {
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int QP = F32 ? 3 : 1, PP = F32 ? 3 : 2;
   constexpr int NT = 4 * NCH;  // 16-column tiles of the output

@@ -112,6 +112,16 @@ def test_attention_refusals():
         assert lib.epicache_kv8_attention(ctypes.byref(prm), ctypes.byref(cache), A, None, 0, A, A, A, 1 << 40, None) == status, field
 
 
+def test_too_many_queries():
+    for kw in (dict(patch_len=(1 << 18) + 1), dict(patch_len=1 << 18, n_batch=30000)):
+        prm, cache = fixture(causal_patch=0, n_cached=0, n_block=1)
+        for name, val in kw.items():
+            setattr(prm, name, val)
+        prm.q_stride_h, prm.q_stride_b = 1 << 25, 1 << 29
+        cache.stride_b, cache.scale_stride_b, cache.row_stride_b = 1 << 20, 1 << 10, 1 << 10
+        assert ep.load().epicache_kv8_attention(ctypes.byref(prm), ctypes.byref(cache), A, None, 0, A, A, A, 1 << 40, None) == ep.ERR_UNSUPPORTED
+
+
 def test_evict_refusals():
     lib, (prm, cache) = ep.load(), fixture()
     p, c = ctypes.byref(prm), ctypes.byref(cache)
@@ -147,6 +157,6 @@ def test_make_kv8_refuses_what_does_not_belong_together():
     ep.make_kv8(k.view(torch.uint8), v.view(torch.uint8), ks, vs, 16)
     for bad in ((k.float(), v.float(), ks, vs, 16, w, pos), (k, v[:, :, :48], ks, vs, 16, w, pos), (k, v, ks, vs, 32, w, pos),
                 (k, v, ks.double(), vs.double(), 16, w, pos), (k, v, ks, vs, 16, w[:, :1], pos), (k, v, ks, vs, 16, w.double(), pos),
-                (k, v, ks, vs, 16, w, pos.long()), (k.transpose(2, 3), v.transpose(2, 3), ks, vs, 16, w, pos)):
+                (k, v, ks, vs, 16, w, pos.long()), (k, v, ks, vs, 16, w.to("meta"), pos), (k.transpose(2, 3), v.transpose(2, 3), ks, vs, 16, w, pos)):
         with pytest.raises(ValueError):
             ep.make_kv8(*bad)
