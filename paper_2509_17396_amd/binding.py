@@ -453,20 +453,25 @@ def alloc_kv8_workspace(params: Params, kv8: Kv8, device="cuda") -> torch.Tensor
     return torch.empty(max(epicache_kv8_workspace_size(params, kv8), 256), dtype=torch.uint8, device=device)
 
 
+def _address(t: Optional[torch.Tensor]):
+    """As _ptr, a plain number: a decoding step's calls are a few us each, and an object for every pointer is a third of one."""
+    return None if t is None else t.data_ptr()
+
+
 def epicache_kv8_append(params: Params, kv8: Kv8, k_new, v_new, n_ctx=None, first_position=None) -> None:
-    _check(load().epicache_kv8_append(ctypes.byref(params), ctypes.byref(kv8), _ptr(k_new), _ptr(v_new), _ptr(n_ctx),
-                                      _ptr(first_position), _stream()), "epicache_kv8_append")
+    _check(load().epicache_kv8_append(ctypes.byref(params), ctypes.byref(kv8), _address(k_new), _address(v_new), _address(n_ctx),
+                                      _address(first_position), _stream()), "epicache_kv8_append")
 
 
 def epicache_kv8_attention(params: Params, kv8: Kv8, q, n_ctx, out, lse_out, workspace, accumulate: bool = False) -> None:
-    _check(load().epicache_kv8_attention(ctypes.byref(params), ctypes.byref(kv8), _ptr(q), _ptr(n_ctx), int(accumulate),
-                                         _ptr(out), _ptr(lse_out), _ptr(workspace),
+    _check(load().epicache_kv8_attention(ctypes.byref(params), ctypes.byref(kv8), _address(q), _address(n_ctx), int(accumulate),
+                                         _address(out), _address(lse_out), _address(workspace),
                                          0 if workspace is None else workspace.numel(), _stream()), "epicache_kv8_attention")
 
 
 def epicache_kv8_evict(params: Params, kv8: Kv8, n_recent: int, n_ctx, budgets, n_kept, workspace, row_from=None) -> None:
-    _check(load().epicache_kv8_evict(ctypes.byref(params), ctypes.byref(kv8), int(n_recent), _ptr(n_ctx), _ptr(budgets),
-                                     _ptr(n_kept), _ptr(row_from), _ptr(workspace), workspace.numel(), _stream()),
+    _check(load().epicache_kv8_evict(ctypes.byref(params), ctypes.byref(kv8), int(n_recent), _address(n_ctx), _address(budgets),
+                                     _address(n_kept), _address(row_from), _address(workspace), workspace.numel(), _stream()),
            "epicache_kv8_evict")
 
 

@@ -267,7 +267,8 @@ __device__ __forceinline__ void move_block(const Kv8Plan& pl, int b, int h, cons
 
 // Which rows stay, and which row takes the place of one that goes.  One workgroup of NW waves per head; VPT keys per thread in
 // registers, or (VPT = 0) made again in every sweep where the rows are too many.
-// Leaves the moves and n_kept.  FUSED: makes the moves as well, a wave per block, and row_from_opt; the lists stay in LDS if they fit.
+// Leaves the moves and n_kept.  FUSED, for at most kFewMoves moves: makes them as well, a wave per block, and row_from_opt.
+constexpr int kFewMoves = 64;  // a lane for each
 template <int VPT, int NW, bool FUSED>
 __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t* __restrict__ budgets, int32_t* n_kept,
                                                       int32_t* row_from_opt, Moves mv) {
@@ -278,7 +279,7 @@ __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t*
   __shared__ uint32_t hist[kHeld ? 1 : 256];
   __shared__ uint32_t wave_a[NW], wave_b[NW];
   __shared__ int wave_latest[NW];
-  __shared__ int32_t near_holes[FUSED ? 64 : 1], near_sources[FUSED ? 64 : 1];
+  __shared__ int32_t near_holes[FUSED ? kFewMoves : 1], near_sources[FUSED ? kFewMoves : 1];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.x, b = kv8_batch_of(pl, bh), h = bh - b * pl.Hkv;
@@ -298,12 +299,13 @@ __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t*
   if (K == n || K == 0) {  // all stay, or none
     if (out)
       for (int i = tid; i < mv.pitch; i += NW * 64) out[i] = i < K ? i : -1;
-    for (int i = tid; i <= mv.blocks; i += NW * 64) starts[i] = 0;
+    if (!FUSED)
+      for (int i = tid; i <= mv.blocks; i += NW * 64) starts[i] = 0;
     if (tid == 0) n_kept[bh] = K;
     return;
   }
   const float2 cut = make_float2(k_scale[K >> shift], v_scale[K >> shift]);
-  if (tid == 0) mv.cut[bh] = cut;
+  if (!FUSED && tid == 0) mv.cut[bh] = cut;
 
   const int groups = kHeld ? VPT : (n + NW * 64 - 1) / (NW * 64);  // 64-wide groups per wave
   const int base = wave * groups * 64 + lane;
@@ -428,8 +430,7 @@ __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t*
     moves += wave_a[x];
   }
   const uint32_t holes_first = holes;
-  const bool near = FUSED && moves <= 64;
-  if (near) holes_of = near_holes, sources_of = near_sources;
+  if (FUSED) holes_of = near_holes, sources_of = near_sources;
   each_row([&](int i, bool stays) {
     const int first = i - lane;  // rows first .. first + 63 here: all on one side of K, but for the ones around it
     if (first < K) {
@@ -437,7 +438,7 @@ __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t*
       const uint64_t mask = __ballot(hole);
       const uint32_t before = holes + lanes_below(mask);
       if (hole) holes_of[before] = i;
-      if (!near && i < K && (i & ((1 << shift) - 1)) == 0) starts[i >> shift] = (int32_t)before;
+      if (!FUSED && i < K && (i & ((1 << shift) - 1)) == 0) starts[i >> shift] = (int32_t)before;
       holes += __popcll(mask);
     }
     if (first + 64 > K) {
@@ -447,11 +448,10 @@ __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t*
       sources += __popcll(mask);
     }
   });
-  if (!near)
+  if (!FUSED)
     for (int i = kept_blocks + tid; i <= mv.blocks; i += NW * 64) starts[i] = (int32_t)moves;
   if (tid == 0) n_kept[bh] = K;
   if constexpr (FUSED) {
-    if (!near) __threadfence_block();
     __syncthreads();
     if (out) {
       uint32_t before = holes_first;
@@ -464,27 +464,22 @@ __global__ __launch_bounds__(NW * 64) void kv8_choose(Kv8Plan pl, const int32_t*
       for (int i = K + tid; i < mv.pitch; i += NW * 64) out[i] = -1;
     }
     if (!kHeld) __syncthreads();  // the keys have been made for the last time: weights may change
-    if (near) {  // a wave per block that takes rows in
-      const int block_of = lane < (int)moves ? near_holes[lane] >> shift : -1;
-      const int before = lane == 0 ? -2 : near_holes[max(lane - 1, 0)] >> shift;
-      uint64_t firsts = __ballot(lane < (int)moves && block_of != before);
-      for (int x = 0; firsts != 0; x++) {
-        const int first = __ffsll((unsigned long long)firsts) - 1;
-        firsts &= firsts - 1;
-        if (x % NW != wave) continue;
-        const int end = firsts ? __ffsll((unsigned long long)firsts) - 1 : (int)moves;
-        move_block(pl, b, h, near_holes, near_sources, first, end, __builtin_amdgcn_readlane(block_of, first), K, cut, lane);
-      }
-    } else {
-      for (int block = wave; block < kept_blocks; block += NW)
-        if (starts[block] != starts[block + 1])
-          move_block(pl, b, h, holes_of, sources_of, starts[block], starts[block + 1], block, K, cut, lane);
+    // a wave per block that takes rows in
+    const int block_of = lane < (int)moves ? near_holes[lane] >> shift : -1;
+    const int before = lane == 0 ? -2 : near_holes[max(lane - 1, 0)] >> shift;
+    uint64_t firsts = __ballot(lane < (int)moves && block_of != before);
+    for (int x = 0; firsts != 0; x++) {
+      const int first = __ffsll((unsigned long long)firsts) - 1;
+      firsts &= firsts - 1;
+      if (x % NW != wave) continue;
+      const int end = firsts ? __ffsll((unsigned long long)firsts) - 1 : (int)moves;
+      move_block(pl, b, h, near_holes, near_sources, first, end, __builtin_amdgcn_readlane(block_of, first), K, cut, lane);
     }
   }
 }
 
 // The moves, a wave per block, and row_from_opt.
-constexpr int kMoveWaves = 4, kFewMoves = 64;
+constexpr int kMoveWaves = 4;
 __global__ __launch_bounds__(kMoveWaves * 64) void kv8_move(Kv8Plan pl, const int32_t* __restrict__ n_kept, int32_t* row_from_opt,
                                                             Moves mv) {
   __shared__ int32_t row_of[kMoveWaves][128];
