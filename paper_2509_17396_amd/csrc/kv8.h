@@ -53,7 +53,6 @@ hipError_t launch_kv8_evict(const Kv8Plan& pl, const int32_t* budgets, int32_t* 
 
 typedef __attribute__((ext_vector_type(2))) float kv8_f32x2;
 
-constexpr float kLargestCode = 448.f;
 constexpr uint32_t kNanCode = 0x7f;
 
 // The smallest power of two, at least 2^-126, by which `amax` (finite) becomes at most 448 = 1.75 * 2^8.

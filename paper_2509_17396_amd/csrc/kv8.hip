@@ -10,7 +10,7 @@
 // take 128 us, kv8_choose 22 of them and kv8_move 106 (4.2 TB/s of what the counters see, scattered rows of 128 bytes).
 #include <hip/hip_bf16.h>
 
-#include <algorithm>
+#include <type_traits>
 
 #include "kv8.h"
 #include "select_util.h"
